@@ -268,6 +268,134 @@ ttf_status ttf_select_threshold(const ttf_params* params, const float* best_sim,
 ttf_status ttf_regate(const ttf_params* params, const void* features, const float* thresholds,
                       void* workspace, size_t workspace_bytes, const ttf_outputs* out, void* hip_stream);
 
+/*
+ * From the compressed rows into attention.
+ *
+ * What a language model does next with the rows, positions and lengths of the pass: norm and rotate queries
+ * and keys by the rows' (t, y, x) positions, put keys and values into a paged cache, attend over it.  Rows are
+ * packed sequence after sequence, as ttf_compress packs clips: row_offsets may be its output, and pos its pos_ids
+ * planes.  dtype, here and there, is a ttf_dtype; sums, norms, angles and softmax statistics are held in 32 bits or more and
+ * every output is rounded once.
+ *
+ * The lengths, offsets, positions and page numbers are device data and are not checked by the host.  Whatever
+ * they hold, nothing outside the buffers described is read or written:
+ *   - row_offsets has to be non-decreasing and start at 0 or later; entries beyond `rows` count as `rows`.  (With
+ *     others the outputs are undefined.)  Rows outside [row_offsets[0], row_offsets[batch]) are left as they were.
+ *   - cached[b] < 0: sequence b appends nothing, and its rows attend to nothing.
+ *   - Page-table entries outside [0, pages) are pages that are not there (not yet given out, or given back behind a
+ *     window), and so is everything beyond table_width: nothing is appended to them, and their keys are left out of the softmax.
+ */
+typedef enum { TTF_ROPE_HALF = 0, TTF_ROPE_INTERLEAVED = 1 } ttf_rope_layout;
+
+/*
+ * Queries, keys and values of `rows` rows, with the norm and the rotation they get.  Strides are in elements; the
+ * entries of a head are contiguous.  Pointers and strides of q, k, v and the outputs are multiples of 16 bytes.
+ *
+ *   norm     y_i = x_i w_i / sqrt(mean_i x_i^2 + eps) over the head_dim entries of a head, where the weight is given
+ *   angle    theta_j = pos[axis[j]][row] * inv_freq[j] for the pairs j < rotary_dim / 2, formed in 64 bits
+ *   rotate   (y_a, y_b) -> (y_a c - y_b s, y_b c + y_a s), c = attention_factor cos theta_j, s = attention_factor sin theta_j,
+ *            (a, b) = (j, j + rotary_dim/2) with TTF_ROPE_HALF, (2j, 2j+1) with TTF_ROPE_INTERLEAVED; entries from
+ *            rotary_dim on are not rotated
+ */
+typedef struct {
+    int32_t dtype;                  /* of q, k, v, the weights and the outputs                                    */
+    int32_t head_dim;               /* D: a multiple of 8, at most 256                                            */
+    int32_t heads, kv_heads;        /* of q; of k and v                                                           */
+    int32_t rows, batch;            /* rows of the buffers; sequences.  Up to 2^24 rows, 2^20 sequences           */
+    const int32_t* row_offsets;     /* [batch+1] first row of every sequence.  ttf_qk_norm_rope: NULL = all rows  */
+    const int32_t* cached;          /* [batch] pairs already in the cache (ttf_cache_append only)                 */
+    const void *q, *k, *v;          /* [rows, heads, D], [rows, kv_heads, D] by the strides                       */
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+    void *q_out, *k_out;            /* may be q and k themselves (same strides), otherwise must not overlap them  */
+    int64_t qo_row, qo_head, ko_row, ko_head;
+    const void *q_weight, *k_weight;   /* [D] norm weights; NULL = no norm                                        */
+    float eps;                      /* >= 0, finite                                                               */
+    int32_t rotary_dim;             /* R: even, 0 <= R <= D; 0 = no rotation (pos and inv_freq may be NULL)       */
+    int32_t layout;                 /* ttf_rope_layout                                                            */
+    int32_t axes;                   /* position planes, 1 to 4                                                    */
+    const double* inv_freq;         /* [R/2]                                                                      */
+    const int32_t* axis;            /* [R/2] plane of every pair, NULL = 0; entries outside [0, axes) count as 0  */
+    const int32_t* pos;             /* [axes, rows] planes pos_stride entries apart                               */
+    int64_t pos_stride;
+    float attention_factor;
+} ttf_qk_params;
+
+/* A paged cache: page p, slot s, head h of k (and of v) starts at element p*page_stride + s*slot_stride +
+ * h*head_stride; entry t of sequence b is slot t % page_size of page page_table[b*table_stride + t / page_size].
+ * Pointers and strides of k and v are multiples of 16 bytes. */
+typedef struct {
+    void *k, *v;
+    const int32_t* page_table;      /* [batch, table_width]                                     */
+    int64_t page_stride, slot_stride, head_stride, table_stride;
+    int32_t pages, page_size, table_width;
+} ttf_kv_cache;
+
+/*
+ * Frequencies of a rotation, host arithmetic on HOST arrays: inv_freq[j] = base^(-2j/R) of the R/2 pairs, R = rotary_dim,
+ * slowed down for contexts longer than the model was trained on (original_length positions):
+ *   TTF_ROPE_PLAIN    as they are
+ *   TTF_ROPE_LINEAR   all divided by factor
+ *   TTF_ROPE_BASE     base * factor^(R/(R-2)) in the place of base: the first pair stays, the last is divided by factor
+ *   TTF_ROPE_PARTS    divided by factor to a share g_j in [0,1]: f (1 - g) + f / factor g, with g growing linearly in j from 0 to 1
+ *                     between the pairs that turn `fast` and `slow` times over original_length positions (the first rounded
+ *                     down, the second up, both kept within 0 .. R/2-1); attention_factor = 0.1 ln(factor) + 1
+ *   TTF_ROPE_TURNS    the same with 1 - g linear in the number of turns between slow and fast; attention_factor = 1
+ * and axis[j], the plane of each pair, from the number of pairs of every plane: sections[axes] (HOST; their sum is R/2; NULL: all
+ * plane 0).  take_turns 0: one block of pairs after the other.  Otherwise the planes take turns: pair j goes to plane
+ * a = j % axes where a > 0 and j / axes < sections[a], else to plane 0 (there have to be that many pairs).
+ * Output pointers may be NULL.  INVALID_ARG: rotary_dim odd or < 2, base <= 1, factor < 1, original_length < 1 where it
+ * is used, slow not below fast, a negative section, sections that do not sum to R/2, axes outside 1..4.
+ */
+typedef enum { TTF_ROPE_PLAIN = 0, TTF_ROPE_LINEAR = 1, TTF_ROPE_BASE = 2, TTF_ROPE_PARTS = 3, TTF_ROPE_TURNS = 4 } ttf_rope_scaling;
+ttf_status ttf_rope_table(int32_t rotary_dim, double base, int32_t scaling, double factor, double original_length, double fast,
+                          double slow, int32_t axes, const int32_t* sections, int32_t take_turns, double* inv_freq,
+                          int32_t* axis, float* attention_factor);
+
+/*
+ * Norm and rotation of queries and keys in one pass: q_out = rotate(norm(q)), k_out = rotate(norm(k)).  q (with heads 0)
+ * or k (with kv_heads 0) may be left out; v is not used.
+ * Errors: INVALID_ARG (NULL pointer, bad sizes, bad strides, eps), UNSUPPORTED (dtype, head_dim, alignment), HIP.
+ */
+ttf_status ttf_qk_norm_rope(const ttf_qk_params* params, void* hip_stream);
+
+/*
+ * The same, with the keys and the values put into the cache: row i of sequence b (row row_offsets[b] + i of the
+ * buffers) becomes entry cached[b] + i.  k_out is not used.  q (heads 0) may be left out; rotated queries go to q_out.
+ * Two rows that the page table sends to one slot leave either's entries there, element by element.
+ * Errors: as above.
+ */
+ttf_status ttf_cache_append(const ttf_qk_params* params, const ttf_kv_cache* cache, void* hip_stream);
+
+/*
+ * Attention of new rows over the cache they were appended to.  Row i of sequence b has index t = cached[b] + i; of the
+ * entries u < cached[b] + row_offsets[b+1] - row_offsets[b] it sees those with u <= t (causal), u > t - window (window > 0),
+ * on pages that are there:
+ *   out = sum_u w_u v_u,  w = softmax_u(scale <q, k_u>),   lse = ln sum_u exp(scale <q, k_u>)
+ * (lse joins parts of a context attended to separately).  A row that sees nothing gets out = 0, lse = -inf.  Query head h reads
+ * key head h / (heads / kv_heads).  Entries that a row does not see have no influence on it, whatever bits
+ * they hold.  Ordinary decoding is the chunk of one row: ttf_decode_alignment's position is cached[b], its mask
+ * length the number of entries seen.
+ *   max_rows    most rows of a sequence, or any other number: it picks the kernel (and so the order of sums), nothing else
+ *   workspace   DEVICE, ttf_attention_workspace_size() bytes, 256-byte aligned; contents on entry do not matter
+ * Errors: INVALID_ARG (NULL pointer, bad sizes, heads no multiple of kv_heads, scale not finite, window < 0), UNSUPPORTED (dtype,
+ * head_dim, alignment), WORKSPACE_TOO_SMALL, HIP.
+ */
+typedef struct {
+    int32_t dtype, head_dim, heads, kv_heads;       /* as in ttf_qk_params                             */
+    int32_t rows, batch, max_rows;
+    int32_t causal, window;                         /* 0 or 1; entries a row looks back over, 0 = all  */
+    float scale;
+    const int32_t* row_offsets;                     /* [batch+1]                                       */
+    const int32_t* cached;                          /* [batch] entries in the cache before these rows  */
+    const void* q;                                  /* [rows, heads, D] by the strides                 */
+    void* out;                                      /* [rows, heads, D] by the strides; may be q       */
+    float* lse;                                     /* optional [rows, heads]                          */
+    int64_t q_row, q_head, o_row, o_head;
+} ttf_attention_params;
+ttf_status ttf_attention_workspace_size(const ttf_attention_params* params, size_t* bytes);
+ttf_status ttf_paged_attention(const ttf_attention_params* params, const ttf_kv_cache* cache, void* workspace,
+                               size_t workspace_bytes, void* hip_stream);
+
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char* ttf_status_string(ttf_status status);
 

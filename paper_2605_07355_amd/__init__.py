@@ -32,3 +32,12 @@ from .binding import (  # noqa: F401
     ttf_profile_enable,
     ttf_profile_read,
 )
+from .serving import (  # noqa: F401
+    TTFKVCache,
+    TTFRope,
+    ttf_rope_table,
+    ttf_qk_norm_rope,
+    ttf_cache_append,
+    ttf_attention_workspace_size,
+    ttf_paged_attention,
+)

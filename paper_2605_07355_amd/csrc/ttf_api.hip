@@ -11,6 +11,7 @@
 #include <utility>
 
 #include "ttf_internal.h"
+#include "ttf_serve.h"
 
 namespace ttf {
 
@@ -264,6 +265,9 @@ ttf_status check_params(const ttf_params* p)
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 }  // namespace
+
+void set_last_hip_error(hipError_t e) { g_last_hip_error = static_cast<int>(e); }
+
 }  // namespace ttf
 
 using namespace ttf;
