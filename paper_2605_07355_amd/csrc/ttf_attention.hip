@@ -14,12 +14,16 @@
 // permutes; product i then holds the entries d = NI c + i, c = 0..15.  So neither K nor V goes through LDS.
 //
 // Few rows are bound by the bytes of the cache: 16 KiB of K and V a wave in flight while the block before is worked on.
+#include <type_traits>
+
 #include "ttf_attend.h"
 
 namespace ttf {
 
 hipError_t launch_attention_join(const ttf_attention_params& p, const ttf_kv_cache& c, int columns, int step, int target,
                                  int width, const float* ws_out, const float* ws_stat, hipStream_t s);
+hipError_t launch_attention_wide(const ttf_attention_params& p, const ttf_kv_cache& c, int width, int target, float* ws_out,
+                                 float* ws_stat, hipStream_t s);
 
 namespace {
 
@@ -486,8 +490,9 @@ namespace {
 
 // The kernel of a call and its sizes.
 struct Choice {
+    bool wide;      // the kernel for many rows
     int width;      // head dimension the kernel is built for
-    int tiles;      // column tiles of 16
+    int columns;    // columns of a tile
     int step;       // keys a workgroup takes a step
     int target;     // workgroups that fill the chip
 };
@@ -497,8 +502,15 @@ Choice choose(const ttf_attention_params& p)
     Choice x;
     x.width = p.head_dim <= 64 ? 64 : p.head_dim <= 128 ? 128 : 256;
     const long long pairs = (long long)(p.max_rows < p.rows ? p.max_rows : p.rows) * (p.heads / p.kv_heads);
-    x.tiles = pairs <= 16 ? 1 : (pairs <= 32 || x.width == 256) ? 2 : 4;
-    if (x.width == 256 && p.dtype == TTF_F32) x.tiles = 1;
+    x.wide = p.dtype == TTF_BF16 && pairs > 32;
+    if (x.wide) {
+        x.columns = 128;
+        x.step = 64;
+        x.target = 512;
+        return x;
+    }
+    x.columns = pairs <= 16 ? 16 : (pairs <= 32 || p.dtype == TTF_BF16) ? 32 : 64;
+    if (x.width == 256 && p.dtype == TTF_F32) x.columns = 16;
     x.step = p.dtype == TTF_BF16 ? 128 : 64;
     x.target = 1024;
     return x;
@@ -519,31 +531,32 @@ hipError_t launch(const ttf_attention_params& p, const ttf_kv_cache& c, const Ch
 size_t attention_workspace_bytes(const ttf_attention_params& p)
 {
     const Choice x = choose(p);
-    return (size_t)2 * x.target * 16 * x.tiles * (x.width + 2) * sizeof(float);
+    return (size_t)2 * x.target * x.columns * (x.width + 2) * sizeof(float);
 }
 
 hipError_t launch_attention(const ttf_attention_params& p, const ttf_kv_cache& c, void* workspace, hipStream_t s)
 {
     const Choice x = choose(p);
-    float *ws_out = static_cast<float*>(workspace), *ws_stat = ws_out + (size_t)2 * x.target * 16 * x.tiles * x.width;
-    hipError_t e;
-    if (p.dtype == TTF_BF16) {
-        if (x.width == 64)
-            e = x.tiles == 1 ? launch<bf16_t, 64, 1>(p, c, x, ws_out, ws_stat, s) : x.tiles == 2 ? launch<bf16_t, 64, 2>(p, c, x, ws_out, ws_stat, s) : launch<bf16_t, 64, 4>(p, c, x, ws_out, ws_stat, s);
-        else if (x.width == 128)
-            e = x.tiles == 1 ? launch<bf16_t, 128, 1>(p, c, x, ws_out, ws_stat, s) : x.tiles == 2 ? launch<bf16_t, 128, 2>(p, c, x, ws_out, ws_stat, s) : launch<bf16_t, 128, 4>(p, c, x, ws_out, ws_stat, s);
-        else
-            e = x.tiles == 1 ? launch<bf16_t, 256, 1>(p, c, x, ws_out, ws_stat, s) : launch<bf16_t, 256, 2>(p, c, x, ws_out, ws_stat, s);
-    } else {
-        if (x.width == 64)
-            e = x.tiles == 1 ? launch<float, 64, 1>(p, c, x, ws_out, ws_stat, s) : x.tiles == 2 ? launch<float, 64, 2>(p, c, x, ws_out, ws_stat, s) : launch<float, 64, 4>(p, c, x, ws_out, ws_stat, s);
-        else if (x.width == 128)
-            e = x.tiles == 1 ? launch<float, 128, 1>(p, c, x, ws_out, ws_stat, s) : x.tiles == 2 ? launch<float, 128, 2>(p, c, x, ws_out, ws_stat, s) : launch<float, 128, 4>(p, c, x, ws_out, ws_stat, s);
-        else
-            e = launch<float, 256, 1>(p, c, x, ws_out, ws_stat, s);
-    }
+    float *ws_out = static_cast<float*>(workspace), *ws_stat = ws_out + (size_t)2 * x.target * x.columns * x.width;
+    const auto few = [&](auto type, auto width) {
+        using T = decltype(type);
+        constexpr int DP = decltype(width)::value;
+        if (x.columns == 16) return launch<T, DP, 1>(p, c, x, ws_out, ws_stat, s);
+        if constexpr (sizeof(T) == 2 || DP < 256) {
+            if (x.columns == 32) return launch<T, DP, 2>(p, c, x, ws_out, ws_stat, s);
+        }
+        if constexpr (sizeof(T) == 4 && DP < 256) return launch<T, DP, 4>(p, c, x, ws_out, ws_stat, s);
+        return hipErrorInvalidValue;                         // (choose() names no other)
+    };
+    const auto of_width = [&](auto type) {
+        if (x.width == 64) return few(type, std::integral_constant<int, 64>());
+        if (x.width == 128) return few(type, std::integral_constant<int, 128>());
+        return few(type, std::integral_constant<int, 256>());
+    };
+    const hipError_t e = x.wide ? launch_attention_wide(p, c, x.width, x.target, ws_out, ws_stat, s)
+                       : p.dtype == TTF_BF16 ? of_width(bf16_t{}) : of_width(float{});
     if (e != hipSuccess) return e;
-    return launch_attention_join(p, c, 16 * x.tiles, x.step, x.target, x.width, ws_out, ws_stat, s);
+    return launch_attention_join(p, c, x.columns, x.step, x.target, x.width, ws_out, ws_stat, s);
 }
 
 }  // namespace ttf
