@@ -33,81 +33,88 @@ __device__ __forceinline__ Sequence sequence_of(const ttf_attention_params& p, c
 }
 
 // How the work is dealt out.  A tile is up to `columns` (row, query head of the key head's group) pairs of one sequence,
-// its work the 32-entry blocks of the sequence's context.  Every tile of a sequence is cut into the same number of parts along the
-// context, so many that no part is longer than `per` blocks, where all parts together are about `target` workgroups.
+// its work the `step`-key steps of the sequence's context.  Every tile of a sequence is cut into the same number of parts along
+// the context, so many that no part is longer than `per` steps, where all parts together are about `target` (a power of two)
+// workgroups.
 //   part id -> key head fastest, then part, then tile, then sequence: workgroups that run together read neighbouring heads
 //   of the same slots.
-// Tiles of more than one part leave (sum, maximum, unnormalised row) of each part in the workspace; `slot` counts those.
+// Tiles of more than one part leave (maximum, sum, unnormalised row) of each part in the workspace, and part 0 a note for the join.
+// Such a part is more than per / 2 steps long on average, so there are at most 2 target of them, and at most `target` such tiles.
 struct Deal {
     int b, tile, part, parts;
-    long long slot;        // first workspace slot of the tile (times kv_heads), where parts > 1
+    int slot;              // first workspace slot of the tile (times kv_heads), where parts > 1
+    int note;              // its number among the tiles of more than one part
 };
+struct JoinNote { int b, tile, parts, slot; };
+struct JoinNotes { int count, pad[3]; JoinNote note[1]; };
 
-__device__ __forceinline__ long long wave_total(long long v)
+// Sum over the lanes up to this one, at VALU rate: within rows of 16, then lane 15 of each row into the next, then lane 31 on.
+__device__ __forceinline__ int wave_prefix(int v)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
-    return v;
-}
-__device__ __forceinline__ long long wave_prefix(long long v, int lane)   // sum over the lanes up to this one
-{
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const long long below = __shfl_up(v, m, 64);
-        if (lane >= m) v += below;
-    }
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr:1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast:15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // row_bcast:31 into rows 2 and 3
     return v;
 }
 
 __device__ __forceinline__ int tiles_of(int rows, int group, int columns)
 {
-    return (int)(((long long)rows * group + columns - 1) / columns);
+    return (int)((unsigned)(rows * group + columns - 1) / (unsigned)columns);    // (rows * heads <= 2^27)
 }
 
-// The deal of unit `unit` (of parts if `by_part`, else of tiles).  Every wave works it out by itself from the lengths: two passes
-// over the batch, 64 sequences at a time.  False where there is no such unit.
-__device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cache& c, int columns, int step, int target, long long unit,
-                                bool by_part, Deal& d)
+// The deal of part `unit`.  Every wave works it out by itself from the lengths, 64 sequences at a time (batches of up to 64
+// read them once).  False where there is no such part.  With `notes`, counts the tiles of more than one part as well.
+__device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cache& c, int columns, int step, int target, int unit,
+                                JoinNotes* notes, Deal& d)
 {
     const int lane = threadIdx.x & 63, group = p.heads / p.kv_heads;
-    const auto blocks = [&](const Sequence& s) { return max(0, (int)(((long long)s.length - s.begin + step - 1) / step)); };
-    long long total = 0;
-    for (int i = 0; i < p.batch; i += 64) {
-        long long work = 0;
-        if (i + lane < p.batch) {
-            const Sequence s = sequence_of(p, c, i + lane);
-            work = (long long)tiles_of(s.rows, group, columns) * blocks(s);
-        }
-        total += wave_total(work);
-    }
-    const long long share = (total * p.kv_heads + target - 1) / target;
-    const int per = (int)max(1ll, min(share, 0x7fffffffll));
-    long long units = 0, slots = 0;
-    for (int i = 0; i < p.batch; i += 64) {
-        int tiles = 0, parts = 1;
+    int tiles = 0, steps = 0;                                // of sequence i + lane
+    const auto look = [&](int i) {
+        tiles = steps = 0;
         if (i + lane < p.batch) {
             const Sequence s = sequence_of(p, c, i + lane);
             tiles = tiles_of(s.rows, group, columns);
-            parts = max(1, (blocks(s) + per - 1) / per);
+            steps = (int)((unsigned)(max(0, s.length - s.begin) + step - 1) / (unsigned)step);
         }
-        const long long mine = (long long)tiles * (by_part ? parts : 1), held = parts > 1 ? (long long)tiles * parts : 0;
-        const long long upto = units + wave_prefix(mine, lane), slots_upto = slots + wave_prefix(held, lane);
-        const unsigned long long after = __ballot(upto > unit);
-        if (after) {
-            const int at = __ffsll(after) - 1;
-            const long long start = __shfl(upto - mine, at, 64);
-            d.b = i + at;
-            d.parts = __shfl(parts, at, 64);
-            const int in = (int)(unit - start);
-            d.tile = by_part ? in / d.parts : in;
-            d.part = by_part ? in - d.tile * d.parts : 0;
-            d.slot = __shfl(slots_upto - held, at, 64) + (long long)d.tile * d.parts;
-            return true;
-        }
-        units = __shfl(upto, 63, 64);
-        slots = __shfl(slots_upto, 63, 64);
+    };
+    double total = 0.0;                                      // (whole numbers below 2^53)
+    for (int i = 0; i < p.batch; i += 64) {
+        look(i);
+        total += wave_sum((double)tiles * steps);
     }
-    return false;
+    const double share = __builtin_ceil(total * p.kv_heads / target);
+    const int per = share < 1.0 ? 1 : share > 1e9 ? 1000000000 : (int)share;
+    int units = 0, slots = 0, split = 0;
+    bool found = false;
+    for (int i = 0; i < p.batch; i += 64) {
+        if (p.batch > 64) look(i);
+        const int parts = max(1, (int)((unsigned)(steps + per - 1) / (unsigned)per)), mine = tiles * parts;
+        const int upto = units + wave_prefix(mine), held = parts > 1 ? mine : 0, notes_held = parts > 1 ? tiles : 0;
+        const int slots_upto = slots + wave_prefix(held), split_upto = split + wave_prefix(notes_held);
+        const unsigned long long after = __ballot(upto > unit);
+        if (after && !found) {
+            const int at = __builtin_amdgcn_readfirstlane(__ffsll(after) - 1);
+            const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+            d.b = i + at;
+            d.parts = of(parts);
+            const int in = unit - of(upto - mine);
+            if ((unsigned)in >= (unsigned)of(mine)) return false;    // (sums past 32 bits: offsets that make no sense)
+            d.tile = in / d.parts;
+            d.part = in - d.tile * d.parts;
+            d.slot = of(slots_upto - held) + d.tile * d.parts;
+            d.note = of(split_upto - notes_held) + d.tile;
+            found = true;
+            if (!notes) return true;
+        }
+        units = __builtin_amdgcn_readlane(upto, 63);
+        slots = __builtin_amdgcn_readlane(slots_upto, 63);
+        split = __builtin_amdgcn_readlane(split_upto, 63);
+    }
+    if (notes && threadIdx.x == 0) notes->count = split;
+    return found;
 }
 
 }  // namespace ttf

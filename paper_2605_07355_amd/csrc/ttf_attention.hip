@@ -20,34 +20,12 @@
 
 namespace ttf {
 
-hipError_t launch_attention_join(const ttf_attention_params& p, const ttf_kv_cache& c, int columns, int step, int target,
-                                 int width, const float* ws_out, const float* ws_stat, hipStream_t s);
-hipError_t launch_attention_wide(const ttf_attention_params& p, const ttf_kv_cache& c, int width, int target, float* ws_out,
-                                 float* ws_stat, hipStream_t s);
+hipError_t launch_attention_wide(const ttf_attention_params& p, const ttf_kv_cache& c, int width, int target, unsigned grid, float* ws_out,
+                                 float2* ws_stat, JoinNotes* notes, hipStream_t s);
 
 namespace {
 
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-
-template <typename T> constexpr int kBlockTiles = sizeof(T) == 2 ? 2 : 1;    // 16-key tiles a wave works on at once
-
-template <typename T>
-__device__ __forceinline__ void store_row_chunk(T* to, const float* v, int n);   // n % 4 == 0
-template <>
-__device__ __forceinline__ void store_row_chunk<float>(float* to, const float* v, int n)
-{
-    for (int i = 0; i < n; i += 4) *reinterpret_cast<float4*>(to + i) = float4{v[i], v[i + 1], v[i + 2], v[i + 3]};
-}
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
-}
-template <>
-__device__ __forceinline__ void store_row_chunk<bf16_t>(bf16_t* to, const float* v, int n)
-{
-    for (int i = 0; i < n; i += 4)
-        *reinterpret_cast<uint2*>(to + i) = uint2{pack_bf16(v[i], v[i + 1]), pack_bf16(v[i + 2], v[i + 3])};
-}
 
 // Whether a 32-bit word holds an infinite or NaN value (one fp32, or either of two bf16).
 template <typename T>
@@ -57,27 +35,42 @@ __device__ __forceinline__ bool not_finite(uint32_t w)
     return (w & 0x7f800000u) == 0x7f800000u || (w & 0x7f80u) == 0x7f80u;
 }
 
+template <typename T> constexpr int kBlockTiles = sizeof(T) == 2 ? 2 : 1;    // 16-key tiles a wave works on at once
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+// Four values to memory in one access, rounded to T.
+__device__ __forceinline__ void store4(float* to, const float* v) { *reinterpret_cast<float4*>(to) = float4{v[0], v[1], v[2], v[3]}; }
+__device__ __forceinline__ void store4(bf16_t* to, const float* v)
+{
+    *reinterpret_cast<uint2*>(to) = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+}
+
 // A workgroup of four waves works on one part of one tile for one key head; its waves take turns with the blocks of
 // 16 or 32 keys, and their (m, l, O) are joined in LDS at the end.
-//   DP     head dimension rounded up to 64, 128 or 256;  NM  column tiles of 16
-//   WHOLE  pages hold whole 16-key tiles: a tile's address is one for all its keys.  Otherwise every key's page is looked up.
-template <typename T, int DP, int NM, bool WHOLE>
-__global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_cache c, int target, float* ws_out, float* ws_stat)
+//   DP     head dimension rounded up to 64, 128 or 256;  NM  column tiles of 16;  WAVES  a SIMD has registers for
+//   WHOLE  pages hold whole 16-key tiles: a tile's address is one for all its keys, and only a lane's place in it goes by vector
+//          registers.  Otherwise every key's page is looked up.
+//   CUT    the head is shorter than DP: lanes past its end read its start, and take 0
+template <typename T, int DP, int NM, bool WHOLE, bool CUT, int WAVES>
+__global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, ttf_kv_cache c, int target, float* ws_out,
+                                                       float2* ws_stat, JoinNotes* notes)
 {
     constexpr int E = sizeof(T), TILES = kBlockTiles<T>, KB = 16 * TILES, COLUMNS = 16 * NM;
     constexpr int KS = DP * E / 64;                          // 16-byte pieces of K a lane holds per tile
     constexpr int NI = DP / 16, VW = NI * E / 4;             // entries of V, in 32-bit words, a lane holds per key
     constexpr int PAD = DP + 4;
-    constexpr int JOIN = 4 * 16 * PAD, WEIGHTS = 4 * KB * COLUMNS;
-    __shared__ __attribute__((aligned(16))) float lds[JOIN > WEIGHTS ? JOIN : WEIGHTS];
-    __shared__ float stat[2][4][COLUMNS];
+    __shared__ __attribute__((aligned(16))) float lds[4 * 16 * PAD];
+    __shared__ float2 stat[4][COLUMNS];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, m = lane & 15;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, m = lane & 15;
     const int head = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads;
     Deal d;
-    if (!deal_out(p, c, COLUMNS, 4 * KB, target, blockIdx.x / p.kv_heads, true, d)) return;
+    if (!deal_out(p, c, COLUMNS, 4 * KB, target, blockIdx.x / p.kv_heads, blockIdx.x == 0 ? notes : nullptr, d)) return;
     const Sequence seq = sequence_of(p, c, d.b);
-    const int pairs = seq.rows * group, col0 = d.tile * COLUMNS;   // (rows * heads is bounded by the host)
+    const int pairs = seq.rows * group, col0 = d.tile * COLUMNS;
 
     // the columns of this lane, and what they see: entries lower <= u < limit
     int limit[NM], lower[NM];
@@ -92,12 +85,11 @@ __global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_c
         const bool is = pair < pairs;
         limit[n] = is ? limit_of(row) : 0x7fffffff;
         lower[n] = is ? lower_of(row) : 0;
-        const long long h = (long long)head * group + pair % group;
-        const T* from = (const T*)p.q + (seq.first + row) * p.q_row + h * p.q_head;
+        const T* from = (const T*)p.q + (seq.first + row) * p.q_row + ((long long)head * group + pair % group) * p.q_head;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             const int at = (s * 64 + g * 16) / E;
-            q[n][s] = is && at < p.head_dim ? *reinterpret_cast<const u32x4*>(from + at) : u32x4{0, 0, 0, 0};
+            q[n][s] = is && (!CUT || at < p.head_dim) ? *reinterpret_cast<const u32x4*>(from + at) : u32x4{0, 0, 0, 0};
         }
     }
     // what all and what any of the tile's rows see (rows in ascending order: so are their limits)
@@ -106,6 +98,7 @@ __global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_c
     const int begin = lower_of(row_a) & ~31;
     const int steps = max(0, (int)(((long long)any_limit - begin + 4 * KB - 1) / (4 * KB)));
     const int step0 = (int)((long long)steps * d.part / d.parts), step1 = (int)((long long)steps * (d.part + 1) / d.parts);
+    const auto base_of = [&](int step) { return begin + (step * 4 + wave) * KB; };
 
     float top[NM], sum[NM];                                  // m and this lane's share of l
     f32x4 o[NM][NI];
@@ -117,87 +110,87 @@ __global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_c
         for (int i = 0; i < NI; ++i) o[n][i] = f32x4{0, 0, 0, 0};
     }
 
-    const T *kc = (const T*)c.k + head * c.head_stride, *vc = (const T*)c.v + head * c.head_stride;
-    const int32_t* table = c.page_table + d.b * c.table_stride;
     // element offset of entry u's slot, -1 where there is none
+    const int32_t* table = c.page_table + d.b * c.table_stride;
     const auto slot_of = [&](int u) -> long long {
         if (u >= seq.length) return -1;                      // (so u / page_size < table_width)
         const unsigned at = (unsigned)u / (unsigned)c.page_size;
         const int page = table[at];
         return page >= 0 && page < c.pages ? page * c.page_stride + (u - (int)at * c.page_size) * c.slot_stride : -1;
     };
-    const auto base_of = [&](int step) { return begin + (step * 4 + wave) * KB; };
 
-    // WHOLE: lane j holds the offset of tile j % TILES of step `held` + j / TILES; a new set every 64 / TILES steps
+    // Where the keys of a step lie.  WHOLE: lane j holds the offset of tile j % TILES of the j / TILES-th step from the last
+    // refill on, every 64 / TILES steps, and `tile` those of the step at hand, in scalar registers.  Otherwise lane j holds key j % KB's.
+    struct Place { long long tile[WHOLE ? TILES : 1]; };
     long long mine = -1;
-    struct Block { u32x4 k[TILES][KS]; uint32_t v[4 * TILES][VW]; bool there[TILES]; unsigned bad; };
-    const float factor = p.scale * kLog2e;
-
-    const auto fetch = [&](int step, Block& x) {
-        const int base = base_of(step);
-        long long ko[TILES], vo[4 * TILES];
-        x.bad = 0;                                           // bit j: key slot j of this lane is not there
+    const auto locate = [&](int step) -> Place {
+        Place x;
         if constexpr (WHOLE) {
-            if ((step - step0) % (64 / TILES) == 0) mine = slot_of(base_of(step + lane / TILES) + lane % TILES * 16);
+            const int j = (step - step0) % (64 / TILES);
+            if (j == 0) mine = slot_of(base_of(step + lane / TILES) + lane % TILES * 16);
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                const int j = (step - step0) % (64 / TILES) * TILES + t;
-                const long long at = ((long long)__builtin_amdgcn_readlane((int)(mine >> 32), j) << 32) |
-                                     (uint32_t)__builtin_amdgcn_readlane((int)mine, j);
-                x.there[t] = at >= 0;
-                if (at < 0) x.bad |= 15u << 4 * t;
-                const long long tile = at >= 0 ? at : 0;
-                ko[t] = tile + m * c.slot_stride;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) vo[4 * t + r] = tile + (4 * g + r) * c.slot_stride;
-            }
+            for (int t = 0; t < TILES; ++t)
+                x.tile[t] = (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(mine >> 32), j * TILES + t) << 32 |
+                                        (unsigned)__builtin_amdgcn_readlane((int)mine, j * TILES + t));
         } else {
-            const long long at = slot_of(base + lane % KB);
-#pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                x.there[t] = __ballot(at < 0) == 0;
-                ko[t] = max(0ll, __shfl(at, 16 * t + m, 64));
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    vo[4 * t + r] = __shfl(at, 16 * t + 4 * g + r, 64);
-                    if (vo[4 * t + r] < 0) x.bad |= 1u << (4 * t + r);
-                    vo[4 * t + r] = max(0ll, vo[4 * t + r]);
-                }
-            }
+            x.tile[0] = slot_of(base_of(step) + lane % KB);
         }
+        return x;
+    };
+    const char *kc = (const char*)((const T*)c.k + head * c.head_stride), *vc = (const char*)((const T*)c.v + head * c.head_stride);
+    const unsigned slot_bytes = (unsigned)c.slot_stride * E;
+    const unsigned k_at = m * slot_bytes + 16 * g, v_at = 4 * g * slot_bytes + (!CUT || m * NI < p.head_dim ? m * NI * E : 0);
+
+    u32x4 k[TILES][KS];
+    uint32_t v[4 * TILES][VW];
+    const auto fetch_k = [&](const Place& x) {
 #pragma unroll
-        for (int t = 0; t < TILES; ++t)
+        for (int t = 0; t < TILES; ++t) {
+            const char* from;
+            if constexpr (WHOLE) from = kc + max(0ll, x.tile[t]) * E + k_at;
+            else from = kc + max(0ll, __shfl(x.tile[0], 16 * t + m, 64)) * E + 16 * g;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const int at = (s * 64 + g * 16) / E;
-                const bool in = at < p.head_dim;
-                x.k[t][s] = *reinterpret_cast<const u32x4*>(kc + ko[t] + (in ? at : 0));
-                if (!in) x.k[t][s] = u32x4{0, 0, 0, 0};
+                k[t][s] = *reinterpret_cast<const u32x4*>(from + (CUT && (s * 64 + g * 16) / E >= p.head_dim ? 0 : s * 64));
+                if (CUT && (s * 64 + g * 16) / E >= p.head_dim) k[t][s] = u32x4{0, 0, 0, 0};
             }
+        }
+    };
+    const auto fetch_v = [&](const Place& x) {
 #pragma unroll
         for (int j = 0; j < 4 * TILES; ++j) {
+            const char* from;
+            if constexpr (WHOLE) from = vc + max(0ll, x.tile[j / 4]) * E + (j % 4) * slot_bytes + v_at;
+            else from = vc + max(0ll, __shfl(x.tile[0], 16 * (j / 4) + 4 * g + j % 4, 64)) * E + (!CUT || m * NI < p.head_dim ? m * NI * E : 0);
             constexpr int W = VW < 4 ? VW : 4;               // words a load brings
 #pragma unroll
             for (int w = 0; w < VW; w += W) {
-                const int at = m * NI + w * 4 / E;
-                const bool in = at < p.head_dim;
-                const T* from = vc + vo[j] + (in ? at : 0);
+                const bool in = !CUT || m * NI + w * 4 / E < p.head_dim;
                 if constexpr (W == 4) {
-                    const u32x4 y = *reinterpret_cast<const u32x4*>(from);
+                    const u32x4 y = *reinterpret_cast<const u32x4*>(from + (in ? 4 * w : 0));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x.v[j][w + e] = in ? y[e] : 0;
+                    for (int e = 0; e < 4; ++e) v[j][w + e] = in ? y[e] : 0;
                 } else {
                     const u32x2 y = *reinterpret_cast<const u32x2*>(from);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) x.v[j][w + e] = in ? y[e] : 0;
+                    for (int e = 0; e < 2; ++e) v[j][w + e] = in ? y[e] : 0;
                 }
             }
         }
     };
 
-    const auto work = [&](int step, Block& x) {
+    const float factor = p.scale * kLog2e;
+    bool tainted = false;                                    // an infinite or NaN value in a block that not all rows see whole
+    Place now{}, next{};
+    if (step0 < step1) {
+        now = locate(step0);
+        fetch_k(now);
+        fetch_v(now);
+    }
+#pragma unroll 1
+    for (int step = step0; step < step1; ++step) {
+        // K of the next step is on its way as soon as this one's is used up, and so is V
         const int base = base_of(step);
-        if (base >= any_limit) return;
         f32x4 s[NM][TILES];
 #pragma unroll
         for (int n = 0; n < NM; ++n)
@@ -207,34 +200,45 @@ __global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_c
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
                     if constexpr (E == 2) {
-                        a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[t][i]),
+                        a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][i]),
                                                                     __builtin_bit_cast(bf16x8, q[n][i]), a, 0, 0, 0);
                     } else {
-                        const f32x4 y = __builtin_bit_cast(f32x4, x.k[t][i]), z = __builtin_bit_cast(f32x4, q[n][i]);
+                        const f32x4 y = __builtin_bit_cast(f32x4, k[t][i]), z = __builtin_bit_cast(f32x4, q[n][i]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) a = __builtin_amdgcn_mfma_f32_16x16x4f32(y[e], z[e], a, 0, 0, 0);
                     }
                 }
                 s[n][t] = a * factor;
             }
+        if (step + 1 < step1) {
+            next = locate(step + 1);
+            fetch_k(next);
+        }
         bool full = base + KB <= all_limit && base >= all_lower;
+        if constexpr (WHOLE) {
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) full = full && x.there[t];
+            for (int t = 0; t < TILES; ++t) full = full && now.tile[t] >= 0;
+        } else {
+            full = full && !__ballot(now.tile[0] < 0);
+        }
         if (!full) {
+            bool odd = false;
 #pragma unroll
-            for (int t = 0; t < TILES; ++t)
+            for (int j = 0; j < 4 * TILES; ++j) {
+                const int u = base + 16 * (j / 4) + 4 * g + j % 4;
+                bool gone;
+                if constexpr (WHOLE) gone = (now.tile[j / 4] < 0) | (u >= seq.length);
+                else gone = __shfl((int)(now.tile[0] < 0), 16 * (j / 4) + 4 * g + j % 4, 64);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int u = base + 16 * t + 4 * g + r, j = 4 * t + r;
-                    const bool gone = (x.bad >> j & 1) || u >= seq.length;
+                for (int n = 0; n < NM; ++n) s[n][j / 4][j % 4] = (gone | (u >= limit[n]) | (u < lower[n])) ? -INFINITY : s[n][j / 4][j % 4];
+                if (gone) {                                  // whatever the slot holds: weight 0 times that has to be 0
 #pragma unroll
-                    for (int n = 0; n < NM; ++n)
-                        if (gone || u >= limit[n] || u < lower[n]) s[n][t][r] = -INFINITY;
-                    if (gone) {                              // whatever the slot holds: weight 0 times that has to be 0
-#pragma unroll
-                        for (int w = 0; w < VW; ++w) x.v[j][w] = 0;
-                    }
+                    for (int w = 0; w < VW; ++w) v[j][w] = 0;
                 }
+#pragma unroll
+                for (int w = 0; w < VW; ++w) odd |= not_finite<T>(v[j][w]);
+            }
+            tainted |= __ballot(odd) != 0;
         }
         // the maximum moves where a lane's own has gone past it by more than 8
         bool moves = false;
@@ -243,7 +247,7 @@ __global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_c
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) moves = moves || s[n][t][r] > top[n] + 8.0f;
+                for (int r = 0; r < 4; ++r) moves |= s[n][t][r] > top[n] + 8.0f;
         if (__ballot(moves)) {
 #pragma unroll
             for (int n = 0; n < NM; ++n) {
@@ -272,47 +276,6 @@ __global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_c
                     sum[n] += s[n][t][r];
                 }
         }
-        if (!full) {
-            // An infinite or NaN value that some rows see and others do not: 0 times it is no 0, so such a block goes by the
-            // vector units, key by key, and leaves out weights of 0.
-            bool odd = false;
-#pragma unroll
-            for (int j = 0; j < 4 * TILES; ++j)
-#pragma unroll
-                for (int w = 0; w < VW; ++w) odd = odd || not_finite<T>(x.v[j][w]);
-            if (__ballot(odd)) {
-                float* weights = lds + wave * KB * COLUMNS;
-#pragma unroll
-                for (int n = 0; n < NM; ++n)
-#pragma unroll
-                    for (int t = 0; t < TILES; ++t)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) weights[(16 * t + 4 * g + r) * COLUMNS + 16 * n + m] = s[n][t][r];
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll 1
-                for (int u = 0; u < KB; ++u) {
-                    const long long at = slot_of(base + u);
-                    if (at < 0) continue;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int i = 0; i < NI; ++i) {
-                            const int e = (4 * g + r) * NI + i;
-                            const float v = e < p.head_dim ? widen(vc[at + e]) : 0.0f;
-#pragma unroll
-                            for (int n = 0; n < NM; ++n) {
-                                const float weight = weights[u * COLUMNS + 16 * n + m];
-                                if (weight != 0.0f) o[n][i][r] += weight * v;
-                            }
-                        }
-                }
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                return;
-            }
-        }
         if constexpr (E == 2) {
             bf16x8 weight[NM];
 #pragma unroll
@@ -327,7 +290,7 @@ __global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_c
                 u32x4 a;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    a[e] = __builtin_amdgcn_perm(x.v[2 * e + 1][i / 2], x.v[2 * e][i / 2], i % 2 ? 0x07060302u : 0x05040100u);
+                    a[e] = __builtin_amdgcn_perm(v[2 * e + 1][i / 2], v[2 * e][i / 2], i % 2 ? 0x07060302u : 0x05040100u);
 #pragma unroll
                 for (int n = 0; n < NM; ++n)
                     o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), weight[n], o[n][i], 0, 0, 0);
@@ -339,22 +302,67 @@ __global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_c
                 for (int i = 0; i < NI; ++i)
 #pragma unroll
                     for (int n = 0; n < NM; ++n)
-                        o[n][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, x.v[r][i]), s[n][0][r],
-                                                                       o[n][i], 0, 0, 0);
+                        o[n][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v[r][i]), s[n][0][r], o[n][i], 0, 0, 0);
         }
-    };
+        if (step + 1 < step1) {
+            fetch_v(next);
+            now = next;
+        }
+    }
 
-    Block a, b;
-    int step = step0;
-    if (step < step1) fetch(step, a);
+    // An infinite or NaN value that some rows see and others do not: 0 times it is no 0.  Rare, and done over again key by key
+    // on the vector units, which leave out what a column does not see.
+    if (tainted) {
+        asm volatile("" ::: "memory");                       // (keeps this path out of the common one)
+#pragma unroll
+        for (int n = 0; n < NM; ++n) {
+            top[n] = -INFINITY;
+            sum[n] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) o[n][i] = f32x4{0, 0, 0, 0};
+        }
 #pragma unroll 1
-    while (step < step1) {
-        if (step + 1 < step1) fetch(step + 1, b);
-        work(step, a);
-        if (++step >= step1) break;
-        if (step + 1 < step1) fetch(step + 1, a);
-        work(step, b);
-        ++step;
+        for (int x = 0; x < (step1 - step0) * KB; ++x) {
+            const int u = base_of(step0 + x / KB) + x % KB;
+            const long long at = slot_of(u);
+            if (at < 0) continue;
+            const T *kr = reinterpret_cast<const T*>(kc) + at, *vr = reinterpret_cast<const T*>(vc) + at;
+            float y[NI][4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const int e = (4 * g + r) * NI + i;
+                    y[i][r] = widen(vr[!CUT || e < p.head_dim ? e : 0]);
+                }
+#pragma unroll
+            for (int n = 0; n < NM; ++n) {
+                float dot = 0.0f;
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    const int e0 = (s * 64 + g * 16) / E;
+                    if (CUT && e0 >= p.head_dim) continue;
+#pragma unroll
+                    for (int e = 0; e < 16 / E; ++e) {
+                        const uint32_t w = q[n][s][e * E / 4];
+                        const float z = E == 4 ? __builtin_bit_cast(float, w) : __builtin_bit_cast(float, e % 2 ? w & 0xffff0000u : w << 16);
+                        dot = __builtin_fmaf(z, widen(kr[e0 + e]), dot);
+                    }
+                }
+                dot += __shfl_xor(dot, 16, 64);
+                dot += __shfl_xor(dot, 32, 64);
+                if (u >= limit[n] || u < lower[n]) continue;
+                const float score = dot * factor, most = fmaxf(top[n], score);
+                const float by = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top[n] - most);
+                const float weight = __builtin_amdgcn_exp2f(score - (most == -INFINITY ? 0.0f : most));
+                top[n] = most;
+                sum[n] = sum[n] * by + (g == 0 ? weight : 0.0f);
+#pragma unroll
+                for (int i = 0; i < NI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[n][i][r] = o[n][i][r] * by + (weight == 0.0f ? 0.0f : weight * y[i][r]);
+            }
+        }
     }
 
     // join the four waves, one column tile after the other
@@ -362,15 +370,13 @@ __global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_c
     for (int n = 0; n < NM; ++n) {
         sum[n] += __shfl_xor(sum[n], 16, 64);
         sum[n] += __shfl_xor(sum[n], 32, 64);
-        if (g == 0) {
-            stat[0][wave][16 * n + m] = top[n];
-            stat[1][wave][16 * n + m] = sum[n];
-        }
+        if (g == 0) stat[wave][16 * n + m] = float2{top[n], sum[n]};
     }
-    const int tid = threadIdx.x, col = tid >> 4;
+    if (d.parts > 1 && d.part == 0 && head == 0 && threadIdx.x == 0 && d.note < target) notes->note[d.note] = JoinNote{d.b, d.tile, d.parts, d.slot};
+    const int col = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * NI;
 #pragma unroll
     for (int n = 0; n < NM; ++n) {
-        __syncthreads();                                     // (the first one: also the slow blocks' use of the same LDS)
+        __syncthreads();                                     // (the first one: also the rare blocks' use of the same LDS)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -382,109 +388,103 @@ __global__ __launch_bounds__(256) void k_attend(ttf_attention_params p, ttf_kv_c
         if (pair >= pairs) continue;
         float most = -INFINITY, by[4], l = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) most = fmaxf(most, stat[0][w][16 * n + col]);
+        for (int w = 0; w < 4; ++w) most = fmaxf(most, stat[w][16 * n + col].x);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float t = stat[0][w][16 * n + col];
-            by[w] = t == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t - most);
-            l += by[w] * stat[1][w][16 * n + col];           // (a wave without a maximum has summed 0, or NaN)
+            const float2 t = stat[w][16 * n + col];
+            by[w] = t.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t.x - most);
+            l += by[w] * t.y;                                // (a wave without a maximum has summed 0, or NaN)
         }
-        const int e0 = (tid & 15) * NI;
-        float v[NI];
+        float y[NI];
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            v[i] = 0.0f;
+            y[i] = 0.0f;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                if (by[w] != 0.0f) v[i] += by[w] * lds[(w * 16 + col) * PAD + e0 + i];
-            }
+            for (int w = 0; w < 4; ++w)
+                y[i] += by[w] == 0.0f ? 0.0f : by[w] * lds[(w * 16 + col) * PAD + e0 + i];
         }
         if (d.parts > 1) {
-            const long long at = ((d.slot + d.part) * p.kv_heads + head) * COLUMNS + 16 * n + col;
-            if (at >= 2ll * target * COLUMNS) continue;      // (cannot be with offsets that do not decrease)
-            store_row_chunk<float>(ws_out + at * DP + e0, v, NI);
-            if ((tid & 15) == 0) {
-                ws_stat[2 * at] = most;
-                ws_stat[2 * at + 1] = l;
-            }
+            const int at = (d.slot + d.part) * p.kv_heads + head;
+            if ((unsigned)at >= 2u * target) continue;       // (cannot be with offsets that do not decrease)
+            const int row = at * COLUMNS + 16 * n + col;
+#pragma unroll
+            for (int i = 0; i < NI; i += 4) store4(ws_out + (size_t)row * DP + e0 + i, y + i);
+            if ((threadIdx.x & 15) == 0) ws_stat[row] = float2{most, l};
         } else {
             const int row = seq.first + pair / group, h = head * group + pair % group;
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-            for (int i = 0; i < NI; ++i) v[i] *= inv;
+            for (int i = 0; i < NI; ++i) y[i] *= inv;
             T* to = (T*)p.out + row * p.o_row + h * p.o_head;
 #pragma unroll
             for (int i = 0; i < NI; i += 4)
-                if (e0 + i < p.head_dim) store_row_chunk<T>(to + e0 + i, v + i, 4);
-            if (p.lse && (tid & 15) == 0) p.lse[(long long)row * p.heads + h] = l == 0.0f ? -INFINITY : most * kLn2 + logf(l);
+                if (e0 + i < p.head_dim) store4(to + e0 + i, y + i);
+            if (p.lse && (threadIdx.x & 15) == 0) p.lse[(long long)row * p.heads + h] = l == 0.0f ? -INFINITY : most * kLn2 + logf(l);
         }
     }
 }
 
-// Joins the parts of a tile: out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s, in the order of the parts.  A wave per
-// column; the parts' statistics are read 64 at a time.
+// Joins the parts of a tile: out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s, in the order of the parts.  Workgroups go by
+// the notes that the parts' kernel left; a wave takes `each` columns, one after the other.
 template <typename T, int EACH>
-__global__ __launch_bounds__(256) void k_attend_join(ttf_attention_params p, ttf_kv_cache c, int columns, int step, int target,
-                                                     const float* __restrict__ ws_out, const float* __restrict__ ws_stat)
+__global__ __launch_bounds__(256) void k_attend_join(ttf_attention_params p, int columns, int each, int target,
+                                                     const float* __restrict__ ws_out, const float2* __restrict__ ws_stat,
+                                                     const JoinNotes* __restrict__ notes)
 {
-    constexpr int DP = 64 * EACH;
+    constexpr int DP = 64 * EACH, AHEAD = 8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads;
-    Deal d;
-    if (!deal_out(p, c, columns, step, target, blockIdx.x / p.kv_heads, false, d) || d.parts == 1) return;
-    const Sequence seq = sequence_of(p, c, d.b);
-    const int col = blockIdx.y * 4 + wave, pair = d.tile * columns + col;
-    if (pair >= seq.rows * group) return;
-    if (((d.slot + d.parts - 1) * p.kv_heads + head) >= 2ll * target) return;
-    const auto at = [&](int part) { return ((d.slot + part) * p.kv_heads + head) * columns + col; };
-    float most = -INFINITY;
-    for (int s = lane; s < d.parts; s += 64) most = fmaxf(most, ws_stat[2 * at(s)]);
+    const int n = blockIdx.x / p.kv_heads;
+    const JoinNote d = notes->note[n];
+    if (n >= notes->count) return;                           // (what the note holds was not written by this call)
+    if ((unsigned)((d.slot + d.parts - 1) * p.kv_heads + head) >= 2u * target) return;
+    const int2 rows = rows_of(p.row_offsets, d.b, p.rows);
+    for (int x = 0; x < each; ++x) {
+        const int col = (blockIdx.y * 4 + wave) * each + x, pair = d.tile * columns + col;
+        if (pair >= rows.y * group) return;
+        const auto at = [&](int part) { return ((d.slot + part) * p.kv_heads + head) * columns + col; };
+        float most = -INFINITY;
+        for (int s = lane; s < d.parts; s += 64) most = fmaxf(most, ws_stat[at(s)].x);
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) most = fmaxf(most, __shfl_xor(most, x, 64));
-    float l = 0.0f, v[EACH] = {};
-    for (int s0 = 0; s0 < d.parts; s0 += 64) {
-        const int n = min(64, d.parts - s0);
-        float by = 0.0f;
-        if (lane < n) {
-            const float t = ws_stat[2 * at(s0 + lane)], part = ws_stat[2 * at(s0 + lane) + 1];
-            by = t == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t - most);
-            l += by * part;
-        }
-        for (int s = 0; s < n; ++s) {
-            const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, by), s));
-            const float* from = ws_out + at(s0 + s) * DP + lane * EACH;
+        for (int y = 1; y < 64; y <<= 1) most = fmaxf(most, __shfl_xor(most, y, 64));
+        float l = 0.0f, v[EACH] = {};
+        for (int s0 = 0; s0 < d.parts; s0 += 64) {
+            const int parts = min(64, d.parts - s0);
+            float by = 0.0f;
+            if (lane < parts) {
+                const float2 t = ws_stat[at(s0 + lane)];
+                by = t.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t.x - most);
+                l += by * t.y;
+            }
+            for (int s1 = 0; s1 < parts; s1 += AHEAD) {      // (parts past the last: the last again, with a weight of 0)
+                float y[AHEAD][EACH];
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) v[i] += w == 0.0f ? 0.0f : w * from[i];
+                for (int s = 0; s < AHEAD; ++s)
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) y[s][i] = ws_out[(size_t)at(s0 + min(s1 + s, parts - 1)) * DP + lane * EACH + i];
+#pragma unroll
+                for (int s = 0; s < AHEAD; ++s) {
+                    const float w = s1 + s < parts ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, by), s1 + s)) : 0.0f;
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) v[i] += w == 0.0f ? 0.0f : w * y[s][i];
+                }
+            }
         }
+        l = wave_sum(l);
+        const int row = rows.x + pair / group, h = head * group + pair % group;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        T* to = (T*)p.out + row * p.o_row + h * p.o_head + lane * EACH;
+        if (lane * EACH < p.head_dim) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                if constexpr (sizeof(T) == 2) to[i].bits = __builtin_bit_cast(uint16_t, (__bf16)(v[i] * inv));
+                else to[i] = v[i] * inv;
+            }
+        }
+        if (p.lse && lane == 0) p.lse[(long long)row * p.heads + h] = l == 0.0f ? -INFINITY : most * kLn2 + logf(l);
     }
-    l = wave_sum(l);
-    const int row = seq.first + pair / group, h = head * group + pair % group;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    T* to = (T*)p.out + row * p.o_row + h * p.o_head + lane * EACH;
-    if (lane * EACH < p.head_dim) {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            if constexpr (sizeof(T) == 2) to[i].bits = __builtin_bit_cast(uint16_t, (__bf16)(v[i] * inv));
-            else to[i] = v[i] * inv;
-        }
-    }
-    if (p.lse && lane == 0) p.lse[(long long)row * p.heads + h] = l == 0.0f ? -INFINITY : most * kLn2 + logf(l);
 }
 
 }  // namespace
-
-hipError_t launch_attention_join(const ttf_attention_params& p, const ttf_kv_cache& c, int columns, int step, int target,
-                                 int width, const float* ws_out, const float* ws_stat, hipStream_t s)
-{
-    const long long tiles = (long long)p.rows * (p.heads / p.kv_heads) / columns + p.batch;
-    const dim3 grid((unsigned)(tiles * p.kv_heads), (unsigned)(columns / 4));
-    const auto go = [&](auto kernel) {
-        kernel<<<grid, 256, 0, s>>>(p, c, columns, step, target, ws_out, ws_stat);
-        return hipGetLastError();
-    };
-    if (p.dtype == TTF_BF16)
-        return width == 64 ? go(k_attend_join<bf16_t, 1>) : width == 128 ? go(k_attend_join<bf16_t, 2>) : go(k_attend_join<bf16_t, 4>);
-    return width == 64 ? go(k_attend_join<float, 1>) : width == 128 ? go(k_attend_join<float, 2>) : go(k_attend_join<float, 4>);
-}
 
 namespace {
 
@@ -493,8 +493,7 @@ struct Choice {
     bool wide;      // the kernel for many rows
     int width;      // head dimension the kernel is built for
     int columns;    // columns of a tile
-    int step;       // keys a workgroup takes a step
-    int target;     // workgroups that fill the chip
+    int target;     // workgroups that fill the chip, a power of two
 };
 
 Choice choose(const ttf_attention_params& p)
@@ -505,25 +504,61 @@ Choice choose(const ttf_attention_params& p)
     x.wide = p.dtype == TTF_BF16 && pairs > 32;
     if (x.wide) {
         x.columns = 128;
-        x.step = 64;
         x.target = 512;
         return x;
     }
     x.columns = pairs <= 16 ? 16 : (pairs <= 32 || p.dtype == TTF_BF16) ? 32 : 64;
     if (x.width == 256 && p.dtype == TTF_F32) x.columns = 16;
-    x.step = p.dtype == TTF_BF16 ? 128 : 64;
     x.target = 1024;
     return x;
 }
 
-template <typename T, int DP, int NM>
-hipError_t launch(const ttf_attention_params& p, const ttf_kv_cache& c, const Choice& x, float* ws_out, float* ws_stat, hipStream_t s)
+// Workspace: rows of the parts, their statistics, the notes for the join.
+struct Parts {
+    float* out;
+    float2* stat;
+    JoinNotes* notes;
+    size_t bytes;
+};
+
+Parts carve_parts(const Choice& x, void* workspace)
 {
-    const long long tiles = (long long)p.rows * (p.heads / p.kv_heads) / (16 * NM) + p.batch;
-    const unsigned grid = (unsigned)(tiles * p.kv_heads + x.target);
-    if (c.page_size % 16 == 0) k_attend<T, DP, NM, true><<<grid, 256, 0, s>>>(p, c, x.target, ws_out, ws_stat);
-    else k_attend<T, DP, NM, false><<<grid, 256, 0, s>>>(p, c, x.target, ws_out, ws_stat);
+    char* at = static_cast<char*>(workspace);
+    const size_t rows = (size_t)2 * x.target * x.columns, out = rows * x.width * sizeof(float), stat = rows * sizeof(float2);
+    return Parts{reinterpret_cast<float*>(at), reinterpret_cast<float2*>(at + out), reinterpret_cast<JoinNotes*>(at + out + stat),
+                 out + stat + sizeof(JoinNotes) + sizeof(JoinNote) * x.target};
+}
+
+unsigned most_tiles(const ttf_attention_params& p, const Choice& x)
+{
+    return (unsigned)((long long)p.rows * (p.heads / p.kv_heads) / x.columns + p.batch);
+}
+
+template <typename T, int DP, int NM>
+hipError_t launch(const ttf_attention_params& p, const ttf_kv_cache& c, const Choice& x, const Parts& w, hipStream_t s)
+{
+    constexpr int WAVES = NM == 1 && DP * sizeof(T) <= 256 ? 3 : NM * DP * sizeof(T) <= 512 ? 2 : 1;
+    const unsigned grid = most_tiles(p, x) * p.kv_heads + x.target;
+    // (the offsets inside a tile are held in 32 bits)
+    const auto go = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(p, c, x.target, w.out, w.stat, w.notes); };
+    if (c.page_size % 16 != 0 || c.slot_stride >= (1ll << 24)) go(k_attend<T, DP, NM, false, true, WAVES>);
+    else if (p.head_dim < DP) go(k_attend<T, DP, NM, true, true, WAVES>);
+    else go(k_attend<T, DP, NM, true, false, WAVES>);
     return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_join(const ttf_attention_params& p, const Choice& x, const Parts& w, hipStream_t s)
+{
+    // A wave to a column; four to a wave of the many columns of wide tiles, few of which are cut into parts as a rule.
+    const int each = x.columns <= 64 ? 1 : 4;
+    const unsigned tiles = most_tiles(p, x) * p.kv_heads;
+    const dim3 grid(tiles < (unsigned)x.target ? tiles : (unsigned)x.target, (unsigned)(x.columns / 4 / each));
+    const auto go = [&](auto kernel) {
+        kernel<<<grid, 256, 0, s>>>(p, x.columns, each, x.target, w.out, w.stat, w.notes);
+        return hipGetLastError();
+    };
+    return x.width == 64 ? go(k_attend_join<T, 1>) : x.width == 128 ? go(k_attend_join<T, 2>) : go(k_attend_join<T, 4>);
 }
 
 }  // namespace
@@ -531,21 +566,21 @@ hipError_t launch(const ttf_attention_params& p, const ttf_kv_cache& c, const Ch
 size_t attention_workspace_bytes(const ttf_attention_params& p)
 {
     const Choice x = choose(p);
-    return (size_t)2 * x.target * x.columns * (x.width + 2) * sizeof(float);
+    return carve_parts(x, nullptr).bytes;
 }
 
 hipError_t launch_attention(const ttf_attention_params& p, const ttf_kv_cache& c, void* workspace, hipStream_t s)
 {
     const Choice x = choose(p);
-    float *ws_out = static_cast<float*>(workspace), *ws_stat = ws_out + (size_t)2 * x.target * x.columns * x.width;
+    const Parts w = carve_parts(x, workspace);
     const auto few = [&](auto type, auto width) {
         using T = decltype(type);
         constexpr int DP = decltype(width)::value;
-        if (x.columns == 16) return launch<T, DP, 1>(p, c, x, ws_out, ws_stat, s);
+        if (x.columns == 16) return launch<T, DP, 1>(p, c, x, w, s);
         if constexpr (sizeof(T) == 2 || DP < 256) {
-            if (x.columns == 32) return launch<T, DP, 2>(p, c, x, ws_out, ws_stat, s);
+            if (x.columns == 32) return launch<T, DP, 2>(p, c, x, w, s);
         }
-        if constexpr (sizeof(T) == 4 && DP < 256) return launch<T, DP, 4>(p, c, x, ws_out, ws_stat, s);
+        if constexpr (sizeof(T) == 4 && DP < 256) return launch<T, DP, 4>(p, c, x, w, s);
         return hipErrorInvalidValue;                         // (choose() names no other)
     };
     const auto of_width = [&](auto type) {
@@ -553,10 +588,10 @@ hipError_t launch_attention(const ttf_attention_params& p, const ttf_kv_cache& c
         if (x.width == 128) return few(type, std::integral_constant<int, 128>());
         return few(type, std::integral_constant<int, 256>());
     };
-    const hipError_t e = x.wide ? launch_attention_wide(p, c, x.width, x.target, ws_out, ws_stat, s)
+    const hipError_t e = x.wide ? launch_attention_wide(p, c, x.width, x.target, most_tiles(p, x) * p.kv_heads + x.target, w.out, w.stat, w.notes, s)
                        : p.dtype == TTF_BF16 ? of_width(bf16_t{}) : of_width(float{});
     if (e != hipSuccess) return e;
-    return launch_attention_join(p, c, x.columns, x.step, x.target, x.width, ws_out, ws_stat, s);
+    return p.dtype == TTF_BF16 ? launch_join<bf16_t>(p, x, w, s) : launch_join<float>(p, x, w, s);
 }
 
 }  // namespace ttf

@@ -27,6 +27,10 @@ __device__ const uint4 kZeros = {0, 0, 0, 0};
 
 constexpr int kWideColumns = 128, kWideKeys = 64;
 
+// Whether either of two bf16 values is infinite or NaN; one of the two in fp32.
+__device__ __forceinline__ bool not_finite(uint32_t w) { return ((w & 0x7f800000u) == 0x7f800000u) | ((w & 0x7f80u) == 0x7f80u); }
+__device__ __forceinline__ float half_of(uint32_t w, int i) { return __builtin_bit_cast(float, i ? w & 0xffff0000u : w << 16); }
+
 // Number that row r's 16-byte pieces are swapped by.
 template <int DP>
 __device__ __forceinline__ int swizzle(int r)
@@ -37,24 +41,24 @@ __device__ __forceinline__ int swizzle(int r)
 
 template <int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_attention_params p, ttf_kv_cache c, int target, float* ws_out,
-                                                                        float* ws_stat)
+                                                                        float2* ws_stat, JoinNotes* notes)
 {
     constexpr int PIECES = DP / 8, ROW = 2 * DP, HALF = kWideKeys * ROW;       // 16-byte pieces of a row; bytes of a row, of K's block
     constexpr int CALLS = PIECES / 4;                                          // loads of 1 KiB a wave makes for K, and for V
     constexpr int NT = DP / 32, KS = DP / 16;
     __shared__ __attribute__((aligned(1024))) char buf0[2 * HALF], buf1[2 * HALF];
-    __shared__ uint2 taint[2][DP];                           // keys of a block with an infinite value, by entry and sign
-    __shared__ int taken;
+    __shared__ int tainted;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, m = lane & 31;
     const int head = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads;
     Deal d;
-    if (!deal_out(p, c, kWideColumns, kWideKeys, target, blockIdx.x / p.kv_heads, true, d)) return;
+    if (!deal_out(p, c, kWideColumns, kWideKeys, target, blockIdx.x / p.kv_heads, blockIdx.x == 0 ? notes : nullptr, d)) return;
     const Sequence seq = sequence_of(p, c, d.b);
     const int pairs = seq.rows * group;
     // later rows see more keys: they go first
     const int tile = tiles_of(seq.rows, group, kWideColumns) - 1 - d.tile, col0 = tile * kWideColumns;
-    d.slot += (long long)(tile - d.tile) * d.parts;
+    d.slot += (tile - d.tile) * d.parts;
+    if (d.parts > 1 && d.part == 0 && head == 0 && threadIdx.x == 0 && d.note < target) notes->note[d.note] = JoinNote{d.b, tile, d.parts, d.slot};
 
     const auto limit_of = [&](int row) { return p.causal ? (int)min((long long)seq.cached + row + 1, (long long)seq.length) : seq.length; };
     const auto lower_of = [&](int row) {
@@ -133,7 +137,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
 
-    const auto work = [&](const char* block, int base, unsigned long long gone, bool tainted) {
+    const auto work = [&](const char* block, int base, unsigned long long gone) {
         if (base >= any_limit || base + kWideKeys <= any_lower) return;
         f32x16 s[2];
 #pragma unroll
@@ -198,65 +202,19 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
 #pragma unroll
             for (int t = 0; t < NT; ++t)
                 o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(block, i, t), w[i], o[t], 0, 0, 0);
-        if (tainted) {
-            __builtin_amdgcn_sched_barrier(0);
-            asm volatile("" ::: "memory");                   // (keeps this rare path out of the common one)
-            uint32_t weighs[2] = {0, 0};                     // keys that have a weight in this column
+    };
+    // notes an infinite or NaN value in a block that not all rows see whole
+    const auto look = [&](const char* block) {
+        bool odd = false;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const u32x4 x = __builtin_bit_cast(u32x4, w[i]);
+        for (int i = 0; i < HALF / 4096; ++i) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(block + HALF + i * 4096 + threadIdx.x * 16);
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    weighs[i / 2] |= (x[e / 2] & (e % 2 ? 0x7fff0000u : 0x7fffu) ? 1u : 0u) << (16 * (i % 2) + 8 * (e / 4) + e % 4);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                weighs[i] <<= 4 * h;
-                weighs[i] |= __shfl_xor(weighs[i], 32, 64);
-            }
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int e = 32 * t + 8 * (r / 4) + 4 * h + r % 4;
-                    o[t][r] += (taint[0][e].x & weighs[0]) | (taint[0][e].y & weighs[1]) ? INFINITY : 0.0f;
-                    o[t][r] -= (taint[1][e].x & weighs[0]) | (taint[1][e].y & weighs[1]) ? INFINITY : 0.0f;
-                    if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                }
-            }
+            for (int e = 0; e < 4; ++e) odd |= not_finite(v[e]);
         }
+        if (odd) tainted = 1;
     };
-    // An infinite or NaN value that some rows see and others do not: 0 times it is no 0.  Such values are taken out of a block that
-    // not all rows see whole, and noted by sign (NaN: as both); after the product the columns that have a weight for them get them back.
-    const auto take_out = [&](char* block) -> bool {
-#pragma unroll 1
-        for (int i = threadIdx.x; i < HALF / 16; i += 256) {
-            s16x8 v = *reinterpret_cast<const s16x8*>(block + HALF + 16 * i);
-            bool any = false;
-            const int r = i / PIECES, e0 = (i % PIECES ^ swizzle<DP>(r)) * 8;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if ((v[e] & 0x7f80) == 0x7f80) {
-                    const bool nan = v[e] & 0x7f;
-                    for (int sign = 0; sign < 2; ++sign)
-                        if (nan || (v[e] < 0) == (sign == 1)) atomicOr(r < 32 ? &taint[sign][e0 + e].x : &taint[sign][e0 + e].y, 1u << r % 32);
-                    v[e] = 0;
-                    any = true;
-                }
-            if (any) {
-                *reinterpret_cast<s16x8*>(block + HALF + 16 * i) = v;
-                taken = 1;
-            }
-        }
-        __syncthreads();
-        return __builtin_amdgcn_readfirstlane(taken) != 0;
-    };
-
-    const auto clear = [&] {
-        for (int i = threadIdx.x; i < 2 * DP; i += 256) (&taint[0][0])[i] = uint2{0, 0};
-        if (threadIdx.x == 0) taken = 0;
-    };
-    clear();                                                 // (before the first block's barrier)
+    if (threadIdx.x == 0) tainted = 0;                       // (before the first block's barrier)
 
     // two buffers: block n+1 is on its way while block n is worked on; one barrier a block
     if (step0 < step1) {
@@ -273,13 +231,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
                 if (step + 2 < step1) ahead = slot_of(begin + (step + 2) * kWideKeys + lane);
             }
             const int base = begin + step * kWideKeys;
-            const bool tainted = !(base + kWideKeys <= block_limit && base >= block_lower) && take_out(now);
-            work(now, base, gone, tainted);
-            if (tainted) {
-                __syncthreads();
-                clear();
-                __syncthreads();
-            }
+            if (!(base + kWideKeys <= block_limit && base >= block_lower)) look(now);
+            work(now, base, gone);
             gone = gone_next;
         };
 #pragma unroll 1
@@ -289,21 +242,67 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
         }
     }
 
+    __syncthreads();
+    // An infinite or NaN value that some rows see and others do not: 0 times it is no 0.  Rare, and done over again key by key
+    // on the vector units, which leave out what a column does not see.
+    if (__builtin_amdgcn_readfirstlane(tainted)) {
+        asm volatile("" ::: "memory");                       // (keeps this path out of the common one)
+        top = -INFINITY;
+        sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+        const int from = max(begin + step0 * kWideKeys, any_lower), to = min(begin + step1 * kWideKeys, any_limit);
+#pragma unroll 1
+        for (int u = from; u < to; ++u) {
+            const long long at = slot_of(u);
+            if (at < 0) continue;
+            float dot = 0.0f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int e0 = s * 16 + h * 8;
+                if (e0 >= p.head_dim) continue;
+                const u32x4 x = __builtin_bit_cast(u32x4, q[s]), y = *reinterpret_cast<const u32x4*>(kc + at + e0);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    dot = __builtin_fmaf(half_of(x[e / 2], e % 2), half_of(y[e / 2], e % 2), dot);
+            }
+            dot += __shfl_xor(dot, 32, 64);
+            const bool sees = (u < limit) & (u >= lower);
+            const float score = sees ? dot * factor : -INFINITY, most = fmaxf(top, score);
+            const float by = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - most);
+            const float weight = __builtin_amdgcn_exp2f(score - (most == -INFINITY ? 0.0f : most));
+            top = most;
+            sum = sum * by + (h == 0 ? weight : 0.0f);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    const int e0 = 32 * t + 8 * a + 4 * h;
+                    const uint2 y = *reinterpret_cast<const uint2*>(vc + at + (e0 < p.head_dim ? e0 : 0));
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const float v = half_of(b < 2 ? y.x : y.y, b % 2);
+                        o[t][4 * a + b] = o[t][4 * a + b] * by + (weight == 0.0f ? 0.0f : weight * v);
+                    }
+                }
+        }
+    }
+
     sum += __shfl_xor(sum, 32, 64);
     if (!is) return;
     if (d.parts > 1) {
-        const long long at = ((d.slot + d.part) * p.kv_heads + head) * kWideColumns + wave * 32 + m;
-        if (at >= 2ll * target * kWideColumns) return;       // (cannot be with offsets that do not decrease)
+        const int at = (d.slot + d.part) * p.kv_heads + head;
+        if ((unsigned)at >= 2u * target) return;             // (cannot be with offsets that do not decrease)
+        const int part_row = at * kWideColumns + wave * 32 + m;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int a = 0; a < 4; ++a)
-                *reinterpret_cast<float4*>(ws_out + at * DP + 32 * t + 8 * a + 4 * h) =
+                *reinterpret_cast<float4*>(ws_out + (size_t)part_row * DP + 32 * t + 8 * a + 4 * h) =
                     float4{o[t][4 * a], o[t][4 * a + 1], o[t][4 * a + 2], o[t][4 * a + 3]};
-        if (h == 0) {
-            ws_stat[2 * at] = top;
-            ws_stat[2 * at + 1] = sum;
-        }
+        if (h == 0) ws_stat[part_row] = float2{top, sum};
         return;
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -323,14 +322,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
 
 }  // namespace
 
-hipError_t launch_attention_wide(const ttf_attention_params& p, const ttf_kv_cache& c, int width, int target, float* ws_out,
-                                 float* ws_stat, hipStream_t s)
+hipError_t launch_attention_wide(const ttf_attention_params& p, const ttf_kv_cache& c, int width, int target, unsigned grid, float* ws_out,
+                                 float2* ws_stat, JoinNotes* notes, hipStream_t s)
 {
-    const long long tiles = (long long)p.rows * (p.heads / p.kv_heads) / kWideColumns + p.batch;
-    const unsigned grid = (unsigned)(tiles * p.kv_heads + target);
-    if (width == 64) k_attend_wide<64><<<grid, 256, 0, s>>>(p, c, target, ws_out, ws_stat);
-    else if (width == 128) k_attend_wide<128><<<grid, 256, 0, s>>>(p, c, target, ws_out, ws_stat);
-    else k_attend_wide<256><<<grid, 256, 0, s>>>(p, c, target, ws_out, ws_stat);
+    if (width == 64) k_attend_wide<64><<<grid, 256, 0, s>>>(p, c, target, ws_out, ws_stat, notes);
+    else if (width == 128) k_attend_wide<128><<<grid, 256, 0, s>>>(p, c, target, ws_out, ws_stat, notes);
+    else k_attend_wide<256><<<grid, 256, 0, s>>>(p, c, target, ws_out, ws_stat, notes);
     return hipGetLastError();
 }
 
