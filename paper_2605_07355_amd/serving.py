@@ -3,9 +3,9 @@ rotation of queries and keys, cache append, attention over a paged cache.  Argum
 from __future__ import annotations
 
 import ctypes
-import math
+import struct
 from dataclasses import dataclass
-from typing import Optional, Sequence, Tuple
+from typing import Optional, Sequence
 
 import torch
 
@@ -44,6 +44,16 @@ class _AttentionParams(ctypes.Structure):
                 + [(n, _i64) for n in ("q_row", "q_head", "o_row", "o_head")])
 
 
+def _packer(structure):
+    """Packs the fields of a ctypes structure, in order, into bytes of its layout (several times faster than filling it)."""
+    codes = {_i32: "i", _i64: "q", _vp: "P", _f32: "f"}
+    layout = "@" + "".join(codes[kind] for _, kind in structure._fields_)
+    pad = ctypes.sizeof(structure) - struct.calcsize(layout)
+    return struct.Struct(layout + (f"{pad}x" if pad else "")).pack
+
+
+_pack_qk, _pack_cache, _pack_attention = _packer(_QKParams), _packer(_KVCache), _packer(_AttentionParams)
+
 _lib = None
 
 
@@ -69,16 +79,20 @@ def _dtype_of(x: torch.Tensor) -> int:
     return code
 
 
-def _heads(name: str, x: torch.Tensor, like: torch.Tensor) -> None:
-    if x.dim() != 3 or x.stride(2) != 1 and x.shape[2] > 1:
-        raise ValueError(f"{name} must be [rows, heads, head_dim] with contiguous heads")
-    if x.dtype != like.dtype or x.device != like.device or x.shape[2] != like.shape[2] or x.shape[0] != like.shape[0]:
-        raise ValueError(f"{name} must have the rows, head_dim, dtype and device of the other operands")
+def _heads(name: str, x: torch.Tensor, rows: int, D: int, dtype: torch.dtype, gpu: int):
+    """(address, heads, row stride, head stride) of a [rows, heads, D] operand."""
+    shape, strides = x.shape, x.stride()
+    if len(shape) != 3 or shape[0] != rows or shape[2] != D or x.dtype is not dtype or x.get_device() != gpu:
+        raise ValueError(f"{name} must be [rows, heads, head_dim] with the rows, head_dim, dtype and device of the other operands")
+    if strides[2] != 1 and D > 1:
+        raise ValueError(f"{name} must have contiguous heads")
+    return x.data_ptr(), shape[1], strides[0], strides[1]
 
 
-def _ints(name: str, x: torch.Tensor, entries: int, device) -> int:
-    if x.dtype != torch.int32 or x.dim() != 1 or x.numel() != entries or x.device != device or (entries > 1 and x.stride(0) != 1):
-        raise ValueError(f"{name} must be a contiguous int32 [{entries}] tensor on {device}")
+def _vector(name: str, x: torch.Tensor, entries: int, dtype: torch.dtype, gpu: int) -> int:
+    """Address of a contiguous vector."""
+    if x.dtype is not dtype or x.dim() != 1 or x.shape[0] != entries or x.get_device() != gpu or (entries > 1 and x.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous [{entries}] tensor of {dtype} on the operands' device")
     return x.data_ptr()
 
 
@@ -90,16 +104,18 @@ def _empty(shape, dtype, device, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _call(function, device: torch.device, stream, *args) -> None:
-    if not device.type == "cuda":
+def _call(function, gpu: int, stream, *args) -> None:
+    if gpu < 0:
         raise ValueError("tensors must live on the GPU (the library has no CPU path)")
-    if device.index == torch.cuda.current_device():
-        s = torch.cuda.current_stream(device) if stream is None else stream
-        _check(function(*args, s.cuda_stream))
+    if gpu == torch.cuda.current_device():
+        _check(function(*args, _current_stream(gpu) if stream is None else stream.cuda_stream))
     else:
-        with torch.cuda.device(device):
-            s = torch.cuda.current_stream(device) if stream is None else stream
-            _check(function(*args, s.cuda_stream))
+        with torch.cuda.device(gpu):
+            _check(function(*args, _current_stream(gpu) if stream is None else stream.cuda_stream))
+
+
+# address of the current stream, without making a torch.cuda.Stream for it
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda gpu: torch.cuda.current_stream(gpu).cuda_stream)
 
 
 @dataclass
@@ -137,83 +153,73 @@ class TTFKVCache:
     """A paged cache: ``k`` and ``v`` [pages, page_size, kv_heads, head_dim] with contiguous heads and the same
     strides (``transpose(1, 2)`` of a cache that keeps heads first is fine), ``page_table`` int32 [batch, width]."""
 
-    __slots__ = ("k", "v", "page_table", "_struct")
+    __slots__ = ("k", "v", "page_table", "_struct", "_batch", "_heads", "_head_dim", "_gpu")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor):
-        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(3) != 1:
+        shape, strides, gpu = k.shape, k.stride(), k.get_device()
+        if len(shape) != 4 or shape != v.shape or strides != v.stride() or k.dtype is not v.dtype or strides[3] != 1:
             raise ValueError("k and v must be [pages, page_size, kv_heads, head_dim] with contiguous heads, alike in every way")
-        if page_table.dim() != 2 or page_table.dtype != torch.int32 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        if page_table.dim() != 2 or page_table.dtype is not torch.int32 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
             raise ValueError("page_table must be int32 [batch, width] with contiguous rows")
-        if not k.device == v.device == page_table.device:
+        if not gpu == v.get_device() == page_table.get_device():
             raise ValueError("k, v and page_table must live on one device")
         self.k, self.v, self.page_table = k, v, page_table
-        pages, size = k.shape[:2]
-        sp, ss, sh, _ = k.stride()
-        width = page_table.shape[1]
-        stride = page_table.stride(0) if page_table.shape[0] > 1 else width
-        self._struct = _KVCache(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), sp, ss, sh, stride, pages, size, width)
+        pages, size, self._heads, self._head_dim = shape
+        self._batch, width = page_table.shape
+        self._gpu = gpu
+        self._struct = _pack_cache(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), strides[0], strides[1], strides[2],
+                                   page_table.stride(0) if self._batch > 1 else width, pages, size, width)
 
 
-def _qk_params(q, k, v, q_out, k_out, pos, rope, q_weight, k_weight, eps, row_offsets, cached, batch) -> Tuple[_QKParams, torch.device]:
+_NONE = (0, 0, 0, 0)
+
+
+def _qk_params(q, k, v, q_out, k_out, pos, rope, q_weight, k_weight, eps, row_offsets, cached, batch, append):
+    """(packed parameters, device index, rows)."""
     ref = k if k is not None else q
     if ref is None or ref.dim() != 3:
         raise ValueError("q and k must be [rows, heads, head_dim]")
-    rows, _, D = ref.shape
-    device = ref.device
-    p = _QKParams(_dtype_of(ref), D, 0, 0, rows, batch, None, None)
-    if row_offsets is not None:
-        p.row_offsets = _ints("row_offsets", row_offsets, batch + 1, device)
-    if cached is not None:
-        p.cached = _ints("cached", cached, batch, device)
+    (rows, _, D), dtype, gpu = ref.shape, ref.dtype, ref.get_device()
+    code = _dtype_of(ref)
+    qs, qo, ks, ko, vs = _NONE, _NONE, _NONE, _NONE, _NONE
     if q is not None:
-        _heads("q", q, ref)
-        _heads("q_out", q_out, ref)
-        p.heads, p.q, p.q_out = q.shape[1], q.data_ptr(), q_out.data_ptr()
-        p.q_row, p.q_head, _ = q.stride()
-        p.qo_row, p.qo_head, _ = q_out.stride()
-        if q_out.shape[1] != q.shape[1]:
+        qs, qo = _heads("q", q, rows, D, dtype, gpu), _heads("q_out", q_out, rows, D, dtype, gpu)
+        if qs[1] != qo[1]:
             raise ValueError("q_out must have the shape of q")
     if k is not None:
-        _heads("k", k, ref)
-        p.kv_heads, p.k = k.shape[1], k.data_ptr()
-        p.k_row, p.k_head, _ = k.stride()
-        if k_out is not None:
-            _heads("k_out", k_out, ref)
-            if k_out.shape[1] != k.shape[1]:
-                raise ValueError("k_out must have the shape of k")
-            p.k_out = k_out.data_ptr()
-            p.ko_row, p.ko_head, _ = k_out.stride()
-        if v is not None:
-            _heads("v", v, ref)
-            if v.shape[1] != k.shape[1]:
-                raise ValueError("v must have the heads of k")
-            p.v = v.data_ptr()
-            p.v_row, p.v_head, _ = v.stride()
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            if w.dtype != ref.dtype or w.dim() != 1 or w.numel() != D or w.device != device or (D > 1 and w.stride(0) != 1):
-                raise ValueError(f"{name} must be a contiguous [head_dim] tensor of the operands' dtype")
-            setattr(p, name, w.data_ptr())
-    p.eps = eps
+        ks = _heads("k", k, rows, D, dtype, gpu)
+        other = vs = _heads("v", v, rows, D, dtype, gpu) if append else vs
+        if not append:
+            other = ko = _heads("k_out", k_out, rows, D, dtype, gpu)
+        if ks[1] != other[1]:
+            raise ValueError("v and k_out must have the heads of k")
+    rot = layout = axes = freq = axis = where = stride = 0
+    factor = 1.0
     if rope is not None:
-        f, axis = rope.inv_freq, rope.axis
-        if f.dtype != torch.float64 or f.dim() != 1 or f.device != device or (f.numel() > 1 and f.stride(0) != 1):
-            raise ValueError("inv_freq must be a contiguous float64 [rotary_dim / 2] tensor on the operands' device")
-        if pos is None or pos.dtype != torch.int32 or pos.device != device:
-            raise ValueError("pos must be an int32 tensor on the operands' device")
-        if pos.dim() == 1:
-            pos = pos[None]
-        if pos.dim() != 2 or pos.shape[1] < rows or (pos.shape[1] > 1 and pos.stride(1) != 1):
-            raise ValueError("pos must be [axes, rows] (or [rows]), contiguous along the rows")
-        if rope.layout not in _LAYOUTS:
+        pairs = rope.inv_freq.numel()
+        freq = _vector("inv_freq", rope.inv_freq, pairs, torch.float64, gpu)
+        layout = _LAYOUTS.get(rope.layout)
+        if layout is None:
             raise ValueError(f"layout must be one of {tuple(_LAYOUTS)}")
-        p.rotary_dim, p.layout, p.axes = 2 * f.numel(), _LAYOUTS[rope.layout], pos.shape[0]
-        p.inv_freq, p.pos = f.data_ptr(), pos.data_ptr()
-        p.pos_stride = pos.stride(0) if pos.shape[0] > 1 else rows
-        p.attention_factor = rope.attention_factor
-        if axis is not None:
-            p.axis = _ints("axis", axis, f.numel(), device)
-    return p, device
+        if pos is None or pos.dtype is not torch.int32 or pos.get_device() != gpu:
+            raise ValueError("pos must be an int32 tensor on the operands' device")
+        shape, strides = pos.shape, pos.stride()
+        if not 1 <= len(shape) <= 2 or shape[-1] < rows or (shape[-1] > 1 and strides[-1] != 1):
+            raise ValueError("pos must be [axes, rows] (or [rows]), contiguous along the rows")
+        axes = shape[0] if len(shape) == 2 else 1
+        stride = strides[0] if axes > 1 else rows
+        rot, where, factor = 2 * pairs, pos.data_ptr(), rope.attention_factor
+        if rope.axis is not None:
+            axis = _vector("axis", rope.axis, pairs, torch.int32, gpu)
+    packed = _pack_qk(
+        code, D, qs[1], ks[1], rows, batch,
+        0 if row_offsets is None else _vector("row_offsets", row_offsets, batch + 1, torch.int32, gpu),
+        0 if cached is None else _vector("cached", cached, batch, torch.int32, gpu),
+        qs[0], ks[0], vs[0], qs[2], qs[3], ks[2], ks[3], vs[2], vs[3], qo[0], ko[0], qo[2], qo[3], ko[2], ko[3],
+        0 if q_weight is None else _vector("q_weight", q_weight, D, dtype, gpu),
+        0 if k_weight is None else _vector("k_weight", k_weight, D, dtype, gpu),
+        eps, rot, layout, axes, freq, axis, where, stride, factor)
+    return packed, gpu, rows
 
 
 def ttf_qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Optional[torch.Tensor] = None,
@@ -231,9 +237,9 @@ def ttf_qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: 
     if k is not None and k_out is None:
         k_out = _empty(k.shape, k.dtype, k.device, stream)
     batch = max(1, row_offsets.numel() - 1) if row_offsets is not None else 1
-    p, device = _qk_params(q, k, None, q_out, k_out, pos, rope, q_weight, k_weight, eps, row_offsets, None, batch)
-    if p.rows:
-        _call(_library().ttf_qk_norm_rope, device, stream, ctypes.byref(p))
+    packed, gpu, rows = _qk_params(q, k, None, q_out, k_out, pos, rope, q_weight, k_weight, eps, row_offsets, None, batch, False)
+    if rows:
+        _call(_library().ttf_qk_norm_rope, gpu, stream, packed)
     return q_out, k_out
 
 
@@ -244,24 +250,14 @@ def ttf_cache_append(cache: TTFKVCache, k: torch.Tensor, v: torch.Tensor, row_of
                      stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
     """Put normed and rotated keys and the values of packed rows into ``cache``: row i of sequence b becomes entry
     ``cached[b] + i``.  ``q`` is normed and rotated in the same launch.  Returns q_out (None without q)."""
-    batch = cache.page_table.shape[0]
-    if cache.k.dtype != k.dtype or cache.k.device != k.device or tuple(cache.k.shape[2:]) != tuple(k.shape[1:]):
+    if cache.k.dtype is not k.dtype or cache._gpu != k.get_device() or (cache._heads, cache._head_dim) != tuple(k.shape[1:]):
         raise ValueError("the cache must have the heads, head_dim, dtype and device of k")
     if q is not None and q_out is None:
         q_out = _empty(q.shape, q.dtype, q.device, stream)
-    p, device = _qk_params(q, k, v, q_out, None, pos, rope, q_weight, k_weight, eps, row_offsets, cached, batch)
-    if p.rows:
-        _call(_library().ttf_cache_append, device, stream, ctypes.byref(p), ctypes.byref(cache._struct))
+    packed, gpu, rows = _qk_params(q, k, v, q_out, None, pos, rope, q_weight, k_weight, eps, row_offsets, cached, cache._batch, True)
+    if rows:
+        _call(_library().ttf_cache_append, gpu, stream, packed, cache._struct)
     return q_out
-
-
-def _attention_params(q, out, lse, cache, row_offsets, cached, max_rows, scale, causal, window) -> _AttentionParams:
-    rows, heads, D = q.shape
-    sq, so = q.stride(), out.stride()
-    return _AttentionParams(_dtype_of(q), D, heads, cache.k.shape[2], rows, cache.page_table.shape[0],
-                            rows if max_rows is None else max_rows, 1 if causal else 0, window,
-                            D ** -0.5 if scale is None else scale, row_offsets, cached, q.data_ptr(), out.data_ptr(), lse,
-                            sq[0], sq[1], so[0], so[1])
 
 
 def ttf_attention_workspace_size(rows: int, batch: int, heads: int, kv_heads: int, head_dim: int,
@@ -281,31 +277,36 @@ def ttf_paged_attention(q: torch.Tensor, cache: TTFKVCache, row_offsets: torch.T
     rows' own (``ttf_cache_append`` first).  ``max_rows`` (most rows of one sequence; default: all) picks the kernel;
     ``scale`` defaults to 1/sqrt(D); ``window`` > 0: a row looks back over that many entries, itself included; ``lse``
     float32 [rows, heads] is filled where given.  Rows outside ``row_offsets`` stay as they were."""
-    if q.dim() != 3 or q.stride(2) != 1 and q.shape[2] > 1:
-        raise ValueError("q must be [rows, heads, head_dim] with contiguous heads")
-    device = q.device
-    if cache.k.dtype != q.dtype or cache.k.device != device or cache.k.shape[3] != q.shape[2]:
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, heads, head_dim]")
+    (rows, heads, D), dtype, gpu = q.shape, q.dtype, q.get_device()
+    if cache.k.dtype is not dtype or cache._gpu != gpu or cache._head_dim != D:
         raise ValueError("the cache must have the head_dim, dtype and device of q")
-    batch = cache.page_table.shape[0]
-    offsets, have = _ints("row_offsets", row_offsets, batch + 1, device), _ints("cached", cached, batch, device)
     if out is None:
-        out = _empty(q.shape, q.dtype, device, stream)
-    elif out.shape != q.shape or out.dtype != q.dtype or out.device != device or out.stride(2) != 1 and out.shape[2] > 1:
-        raise ValueError("out must be like q, with contiguous heads")
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != tuple(q.shape[:2]) or lse.device != device
+        out = _empty((rows, heads, D), dtype, q.device, stream)
+    at, _, row, head = _heads("q", q, rows, D, dtype, gpu)
+    to, out_heads, out_row, out_head = _heads("out", out, rows, D, dtype, gpu)
+    if out_heads != heads:
+        raise ValueError("out must have the shape of q")
+    if lse is not None and (lse.dtype is not torch.float32 or tuple(lse.shape) != (rows, heads) or lse.get_device() != gpu
                             or not lse.is_contiguous()):
-        raise ValueError("lse must be a contiguous float32 [rows, heads] tensor")
-    if q.shape[0] == 0:
+        raise ValueError("lse must be a contiguous float32 [rows, heads] tensor on the device of q")
+    batch = cache._batch
+    packed = _pack_attention(_dtype_of(q), D, heads, cache._heads, rows, batch, rows if max_rows is None else max_rows,
+                             1 if causal else 0, window, D ** -0.5 if scale is None else scale,
+                             _vector("row_offsets", row_offsets, batch + 1, torch.int32, gpu),
+                             _vector("cached", cached, batch, torch.int32, gpu),
+                             at, to, 0 if lse is None else lse.data_ptr(), row, head, out_row, out_head)
+    if rows == 0:
         return out
-    p = _attention_params(q, out, None if lse is None else lse.data_ptr(), cache, offsets, have, max_rows, scale, causal, int(window))
-    lib, ref = _library(), ctypes.byref(p)
+    lib = _library()
     if workspace is None:
         n = ctypes.c_size_t(0)
-        _check(lib.ttf_attention_workspace_size(ref, ctypes.byref(n)))
-        workspace = _empty(n.value, torch.uint8, device, stream)
-    elif workspace.device != device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        _check(lib.ttf_attention_workspace_size(packed, ctypes.byref(n)))
+        workspace = _empty(n.value, torch.uint8, q.device, stream)
+    elif workspace.get_device() != gpu or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on the device of q")
     base = workspace.data_ptr()
     skip = -base % 256
-    _call(lib.ttf_paged_attention, device, stream, ref, ctypes.byref(cache._struct), base + skip, max(0, workspace.numel() - skip))
+    _call(lib.ttf_paged_attention, gpu, stream, packed, cache._struct, base + skip, max(0, workspace.numel() - skip))
     return out
