@@ -33,18 +33,22 @@ __device__ __forceinline__ Sequence sequence_of(const ttf_attention_params& p, c
 }
 
 // How the work is dealt out.  A tile is up to `columns` (row, query head of the key head's group) pairs of one sequence,
-// its work the `step`-key steps of the sequence's context.  Every tile of a sequence is cut into the same number of parts along
-// the context, so many that no part is longer than `per` steps, where all parts together are about `target` (a power of two)
-// workgroups.
-//   part id -> key head fastest, then part, then tile, then sequence: workgroups that run together read neighbouring heads
-//   of the same slots.
-// Tiles of more than one part leave (maximum, sum, unnormalised row) of each part in the workspace, and part 0 a note for the join.
-// Such a part is more than per / 2 steps long on average, so there are at most 2 target of them, and at most `target` such tiles.
+// its work the blocks of `keys` entries of the sequence's context.  A workgroup's four waves either take turns with the blocks of
+// one key head, or (`neighbours`, where there is enough work) each walk along the same blocks for a key head of its own: then
+// the workgroup reads four neighbouring heads of a slot, 1 KiB where one head is 256 bytes, which the memory likes better.  Every tile of a
+// sequence is cut into the same number of parts along the context, so many that no part is longer than `per` turns, where all parts
+// together are about `target` workgroups (a power of two).
+//   part id -> key head (four of them) fastest, then part, then tile, then sequence.
+// Tiles of more than one part leave (maximum, sum, unnormalised row) of each part and head in the workspace, and part 0 a note for
+// the join.  With n key heads a workgroup, those rows' tiles are at most 2 n target (parts of cut tiles are more than per / 2 turns long
+// on average, also after the last turn of four blocks is rounded up), and the notes at most half as many.
 struct Deal {
     int b, tile, part, parts;
+    int heads;             // key heads of a workgroup: 1 or 4
     int slot;              // first workspace slot of the tile (times kv_heads), where parts > 1
     int note;              // its number among the tiles of more than one part
 };
+constexpr int kNeighbours = 4, kNeighbourTurns = 8;          // least turns a part that make it worth it
 struct JoinNote { int b, tile, parts, slot; };
 struct JoinNotes { int count, pad[3]; JoinNote note[1]; };
 
@@ -65,33 +69,37 @@ __device__ __forceinline__ int tiles_of(int rows, int group, int columns)
     return (int)((unsigned)(rows * group + columns - 1) / (unsigned)columns);    // (rows * heads <= 2^27)
 }
 
-// The deal of part `unit`.  Every wave works it out by itself from the lengths, 64 sequences at a time (batches of up to 64
-// read them once).  False where there is no such part.  With `notes`, counts the tiles of more than one part as well.
-__device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cache& c, int columns, int step, int target, int unit,
-                                JoinNotes* notes, Deal& d)
+// The deal of workgroup `block`.  Every wave works it out by itself from the lengths, 64 sequences at a time (batches of up to 64
+// read them once).  False where nothing is left for it.  With `notes`, counts the tiles of more than one part as well.
+__device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cache& c, int columns, int keys, bool neighbours, int target,
+                                int block, JoinNotes* notes, Deal& d)
 {
     const int lane = threadIdx.x & 63, group = p.heads / p.kv_heads;
-    int tiles = 0, steps = 0;                                // of sequence i + lane
+    int tiles = 0, blocks = 0;                               // of sequence i + lane
     const auto look = [&](int i) {
-        tiles = steps = 0;
+        tiles = blocks = 0;
         if (i + lane < p.batch) {
             const Sequence s = sequence_of(p, c, i + lane);
             tiles = tiles_of(s.rows, group, columns);
-            steps = (int)((unsigned)(max(0, s.length - s.begin) + step - 1) / (unsigned)step);
+            blocks = (int)((unsigned)(max(0, s.length - s.begin) + keys - 1) / (unsigned)keys);
         }
     };
     double total = 0.0;                                      // (whole numbers below 2^53)
     for (int i = 0; i < p.batch; i += 64) {
         look(i);
-        total += wave_sum((double)tiles * steps);
+        total += wave_sum((double)tiles * blocks);
     }
-    const double share = __builtin_ceil(total * p.kv_heads / target);
-    const int per = share < 1.0 ? 1 : share > 1e9 ? 1000000000 : (int)share;
+    // a part of `per` turns: per blocks of one wave and four heads, or 4 per blocks of four waves and one head
+    const double share = __builtin_ceil(total * p.kv_heads / (4.0 * target));
+    const int per = __builtin_amdgcn_readfirstlane(share < 1.0 ? 1 : share > 1e9 ? 1000000000 : (int)share);
+    d.heads = neighbours && per >= kNeighbourTurns ? kNeighbours : 1;
+    const int waves = 4 / d.heads, unit = block / (p.kv_heads / d.heads);
     int units = 0, slots = 0, split = 0;
     bool found = false;
     for (int i = 0; i < p.batch; i += 64) {
         if (p.batch > 64) look(i);
-        const int parts = max(1, (int)((unsigned)(steps + per - 1) / (unsigned)per)), mine = tiles * parts;
+        const int turns = (int)((unsigned)(blocks + waves - 1) / (unsigned)waves);
+        const int parts = max(1, (int)((unsigned)(turns + per - 1) / (unsigned)per)), mine = tiles * parts;
         const int upto = units + wave_prefix(mine), held = parts > 1 ? mine : 0, notes_held = parts > 1 ? tiles : 0;
         const int slots_upto = slots + wave_prefix(held), split_upto = split + wave_prefix(notes_held);
         const unsigned long long after = __ballot(upto > unit);

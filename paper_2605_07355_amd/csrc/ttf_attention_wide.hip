@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, m = lane & 31;
     const int head = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads;
     Deal d;
-    if (!deal_out(p, c, kWideColumns, kWideKeys, target, blockIdx.x / p.kv_heads, blockIdx.x == 0 ? notes : nullptr, d)) return;
+    if (!deal_out(p, c, kWideColumns, kWideKeys / 4, false, target, blockIdx.x, blockIdx.x == 0 ? notes : nullptr, d)) return;
     const Sequence seq = sequence_of(p, c, d.b);
     const int pairs = seq.rows * group;
     // later rows see more keys: they go first

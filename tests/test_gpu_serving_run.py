@@ -204,3 +204,21 @@ def test_shared_pages_and_many_sequences(max_rows):
     ttf.ttf_paged_attention(q.cuda(), ttf.TTFKVCache(k.cuda(), v.cuda(), table.cuda()), _offsets(rows).cuda(), torch.tensor(cached).int().cuda(),
                             max_rows=max_rows, out=out, lse=lse)
     _check_attention(out.cpu(), lse.cpu(), q, ks, vs, rows, cached, True, 0, BF)
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,rows,cached", [
+    (BF, 8, 8, [1, 1, 0, 1, 1], [90001, 1, 400, 70000, 73333]),
+    (BF, 8, 4, [2, 1, 1], [230000, 240000, 17]),
+    (F32, 4, 4, [1, 2], [150000, 100000]),
+])
+def test_long_contexts_side_by_side(dtype, heads, kv_heads, rows, cached):
+    """Contexts so long that workgroups walk along four heads of a slot at once; and the same entries with heads first."""
+    import paper_2605_07355_amd as ttf
+    D, page = 64, 64
+    q, k, v, table, ks, vs = _problem(rows, cached, heads, kv_heads, D, page, dtype)
+    offsets, have = _offsets(rows).cuda(), torch.tensor(cached).int().cuda()
+    for first in (False, True):
+        kg, vg = (t.cuda().transpose(1, 2).contiguous().transpose(1, 2) if first else t.cuda() for t in (k, v))
+        out, lse = torch.full_like(q, 5.0, device="cuda"), torch.full((sum(rows), heads), 5.0, device="cuda")
+        ttf.ttf_paged_attention(q.cuda(), ttf.TTFKVCache(kg, vg, table.cuda()), offsets, have, max_rows=max(rows), out=out, lse=lse)
+        _check_attention(out.cpu(), lse.cpu(), q, ks, vs, rows, cached, True, 0, dtype)
