@@ -47,6 +47,7 @@ struct Deal {
     int heads;             // key heads of a workgroup: 1 or 4
     int slot;              // first workspace slot of the tile (times kv_heads), where parts > 1
     int note;              // its number among the tiles of more than one part
+    Sequence seq;
 };
 constexpr int kNeighbours = 4, kNeighbourTurns = 8;          // least turns a part that make it worth it
 struct JoinNote { int b, tile, parts, slot; };
@@ -76,10 +77,11 @@ __device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cach
 {
     const int lane = threadIdx.x & 63, group = p.heads / p.kv_heads;
     int tiles = 0, blocks = 0;                               // of sequence i + lane
+    Sequence s{};
     const auto look = [&](int i) {
         tiles = blocks = 0;
         if (i + lane < p.batch) {
-            const Sequence s = sequence_of(p, c, i + lane);
+            s = sequence_of(p, c, i + lane);
             tiles = tiles_of(s.rows, group, columns);
             blocks = (int)((unsigned)(max(0, s.length - s.begin) + keys - 1) / (unsigned)keys);
         }
@@ -114,6 +116,7 @@ __device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cach
             d.part = in - d.tile * d.parts;
             d.slot = of(slots_upto - held) + d.tile * d.parts;
             d.note = of(split_upto - notes_held) + d.tile;
+            d.seq = Sequence{of(s.first), of(s.rows), of(s.cached), of(s.length), of(s.begin)};
             found = true;
             if (!notes) return true;
         }

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
     if (!deal_out(p, c, columns, KB, neighbours, target, blockIdx.x, blockIdx.x == 0 ? notes : nullptr, d)) return;
     const int first_head = blockIdx.x % (p.kv_heads / d.heads) * d.heads, waves = 4 / d.heads;    // `waves` share a head
     const int head = first_head + (d.heads > 1 ? wave : 0), turn = d.heads > 1 ? 0 : wave;
-    const Sequence seq = sequence_of(p, c, d.b);
+    const Sequence& seq = d.seq;
     const int col0 = d.tile * columns, pairs = min(seq.rows * group, col0 + columns);   // (pairs of the sequence up to this tile's end)
 
     // the columns of this lane, and what they see: entries lower <= u < limit
@@ -525,7 +525,7 @@ Choice choose(const ttf_attention_params& p)
     if (x.width == 256 && p.dtype == TTF_F32) x.tiles = 1;
     x.columns = pairs < 16 * x.tiles ? (int)pairs : 16 * x.tiles;    // no more than there are: the parts' rows take that much less room
     x.neighbours = p.kv_heads % kNeighbours == 0;
-    x.target = 2048;
+    x.target = 2048 / x.tiles;
     x.slots = 2 * x.target * (x.neighbours ? kNeighbours : 1);
     return x;
 }

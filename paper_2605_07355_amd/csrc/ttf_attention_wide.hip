@@ -27,6 +27,19 @@ __device__ const uint4 kZeros = {0, 0, 0, 0};
 
 constexpr int kWideColumns = 128, kWideKeys = 64;
 
+// 16 bytes a lane from memory straight to LDS: lane l's to byte 16 l from `to` on.  Written out, because the compiler, which cannot tell the
+// buffer being filled from the one being read, would wait for it before every read of LDS.  Whoever reads the bytes has waited for the loads of
+// every wave before (wait_for_loads and a barrier).  No register is written.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"               // (m0 counts as reserved; the compiler puts nothing there that outlives this)
+__device__ __forceinline__ void load_to_lds(unsigned long long from, unsigned to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "m0");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ unsigned lds_offset(const char* p) { return (unsigned)(uintptr_t)(const lds_char*)p; }
+
 // Whether either of two bf16 values is infinite or NaN; one of the two in fp32.
 __device__ __forceinline__ bool not_finite(uint32_t w) { return ((w & 0x7f800000u) == 0x7f800000u) | ((w & 0x7f80u) == 0x7f80u); }
 __device__ __forceinline__ float half_of(uint32_t w, int i) { return __builtin_bit_cast(float, i ? w & 0xffff0000u : w << 16); }
@@ -39,263 +52,68 @@ __device__ __forceinline__ int swizzle(int r)
     return (r & 3) << 2 | (r >> 2 & 3);
 }
 
-template <int DP>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_attention_params p, ttf_kv_cache c, int target, float* ws_out,
-                                                                        float2* ws_stat, JoinNotes* notes)
+// A wave's 32 columns over the entries from .. to - 1 again, key by key on the vector units.
+template <int DP, typename Slot>
+__device__ __forceinline__ void by_keys(int head_dim, const bf16_t* kc, const bf16_t* vc, const Slot& slot_of, int from, int to, int limit,
+                                        int lower, float factor, const bf16x8 (&q)[DP / 16], float& top, float& sum, f32x16 (&o)[DP / 32])
 {
-    constexpr int PIECES = DP / 8, ROW = 2 * DP, HALF = kWideKeys * ROW;       // 16-byte pieces of a row; bytes of a row, of K's block
-    constexpr int CALLS = PIECES / 4;                                          // loads of 1 KiB a wave makes for K, and for V
     constexpr int NT = DP / 32, KS = DP / 16;
-    __shared__ __attribute__((aligned(1024))) char buf0[2 * HALF], buf1[2 * HALF];
-    __shared__ int tainted;
-
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, m = lane & 31;
-    const int head = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads;
-    Deal d;
-    if (!deal_out(p, c, kWideColumns, kWideKeys / 4, false, target, blockIdx.x, blockIdx.x == 0 ? notes : nullptr, d)) return;
-    const Sequence seq = sequence_of(p, c, d.b);
-    const int pairs = seq.rows * group;
-    // later rows see more keys: they go first
-    const int tile = tiles_of(seq.rows, group, kWideColumns) - 1 - d.tile, col0 = tile * kWideColumns;
-    d.slot += (tile - d.tile) * d.parts;
-    if (d.parts > 1 && d.part == 0 && head == 0 && threadIdx.x == 0 && d.note < target) notes->note[d.note] = JoinNote{d.b, tile, d.parts, d.slot};
-
-    const auto limit_of = [&](int row) { return p.causal ? (int)min((long long)seq.cached + row + 1, (long long)seq.length) : seq.length; };
-    const auto lower_of = [&](int row) {
-        return p.window > 0 ? (int)max(0ll, min((long long)seq.cached + row + 1 - p.window, 0x7fffffffll)) : 0;
-    };
-    // this lane's column
-    const int pair = col0 + wave * 32 + m, row = pair / group;
-    const bool is = pair < pairs;
-    const int limit = is ? limit_of(row) : 0x7fffffff, lower = is ? lower_of(row) : 0;
-    const long long qh = (long long)head * group + pair % group;
-    const float factor = p.scale == 0.0f ? 1.0f : fabsf(p.scale) * kLog2e;
-    bf16x8 q[KS];
-    {
-        const bf16_t* from = (const bf16_t*)p.q + (seq.first + row) * p.q_row + qh * p.q_head;
-        const uint32_t flip = p.scale < 0.0f ? 0x80008000u : 0u, keep = p.scale == 0.0f ? 0u : ~0u;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const int at = s * 16 + h * 8;
-            u32x4 y = {0, 0, 0, 0};
-            if (is && at < p.head_dim) y = *reinterpret_cast<const u32x4*>(from + at);
-            q[s] = __builtin_bit_cast(bf16x8, (y ^ flip) & keep);
-        }
-    }
-    // what all and what any of the workgroup's and of this wave's rows see
-    const int row_a = col0 / group, row_z = min(col0 + kWideColumns - 1, pairs - 1) / group;
-    const int begin = lower_of(row_a) & ~31, end = limit_of(row_z);
-    const int steps = max(0, (int)(((long long)end - begin + kWideKeys - 1) / kWideKeys));
-    const int step0 = (int)((long long)steps * d.part / d.parts), step1 = (int)((long long)steps * (d.part + 1) / d.parts);
-    const int wave0 = col0 + wave * 32, wave_row_z = min(wave0 + 31, pairs - 1) / group;
-    const bool wave_is = wave0 < pairs;
-    const int block_limit = limit_of(row_a), block_lower = lower_of(row_z);    // what all rows of the workgroup see
-    const int all_limit = limit_of(wave0 / group), any_limit = wave_is ? limit_of(wave_row_z) : 0;
-    const int all_lower = lower_of(wave_row_z), any_lower = lower_of(wave0 / group);
-
-    // staging: call i of this wave fills the KiB (4 i + wave) of a block
-    const bf16_t *kc = (const bf16_t*)c.k + head * c.head_stride, *vc = (const bf16_t*)c.v + head * c.head_stride;
-    const int32_t* table = c.page_table + d.b * c.table_stride;
-    const auto slot_of = [&](int u) -> long long {           // element offset of entry u's slot, -1 where there is none
-        if (u >= seq.length) return -1;
-        const unsigned at = (unsigned)u / (unsigned)c.page_size;
-        const int page = table[at];
-        return page >= 0 && page < c.pages ? page * c.page_stride + (u - (int)at * c.page_size) * c.slot_stride : -1;
-    };
-    const auto stage = [&](char* to, long long slot) {       // lane l: slot of key l of the block
-#pragma unroll
-        for (int i = 0; i < CALLS; ++i) {
-            const int piece = (4 * i + wave) * 64 + lane, r = piece / PIECES, e = (piece % PIECES ^ swizzle<DP>(r)) * 8;
-            const long long at = __shfl(slot, r, 64);
-            const bool there = at >= 0 && e < p.head_dim;
-            const void* kf = there ? (const void*)(kc + at + e) : (const void*)&kZeros;
-            const void* vf = there ? (const void*)(vc + at + e) : (const void*)&kZeros;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)kf,
-                                             (__attribute__((address_space(3))) void*)(to + (4 * i + wave) * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vf,
-                                             (__attribute__((address_space(3))) void*)(to + HALF + (4 * i + wave) * 1024), 16, 0, 0);
-        }
-    };
-
-    float top = -INFINITY, sum = 0.0f;
-    f32x16 o[NT];
+    const int h = threadIdx.x >> 5 & 1;
+    top = -INFINITY;
+    sum = 0.0f;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
-
-    // V^T of 16 keys by 32 entries: product t, keys 16 s ..
-    const int vr = (lane & 15) >> 2, vc16 = lane >> 4 & 1, low = vc16 * 2 + ((lane & 3) >> 1);
-    const auto v_frag = [&](const char* block, int s, int t) -> bf16x8 {
-        s16x4 part[2];
+#pragma unroll 1
+            for (int u = from; u < to; ++u) {
+                const long long at = slot_of(u);
+                if (at < 0) continue;
+                float dot = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int r = 16 * s + 8 * j + 4 * h + vr;
-            const int at = HALF + r * ROW + (((t * 4 + low) ^ swizzle<DP>(r)) << 4) + (lane & 1) * 8;
-            part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_char*)block + at));
-        }
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-
-    const auto work = [&](const char* block, int base, unsigned long long gone) {
-        if (base >= any_limit || base + kWideKeys <= any_lower) return;
-        f32x16 s[2];
+                for (int s = 0; s < KS; ++s) {
+                    const int e0 = s * 16 + h * 8;
+                    if (e0 >= head_dim) continue;
+                    const u32x4 x = __builtin_bit_cast(u32x4, q[s]), y = *reinterpret_cast<const u32x4*>(kc + at + e0);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < KS; ++i)
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int at = (32 * t + m) * ROW + (((2 * i + h) ^ swizzle<DP>(m)) << 4);
-                const bf16x8 k = *reinterpret_cast<const bf16x8*>(block + at);
-                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[i], s[t], 0, 0, 0);
-            }
-        const bool full = base + kWideKeys <= all_limit && base >= all_lower && gone == 0;
-        if (!full) {
-            // bit k: this column sees the block's key k + 4 h
-            const int from = min(max(lower - base, 0), 64), to = min(max(limit - base, 0), 64);
-            const unsigned long long below = to == 64 ? ~0ull : (1ull << to) - 1, above = from == 64 ? 0ull : ~0ull << from;
-            const unsigned long long sees = (below & above & ~gone) >> (4 * h);
-            const uint32_t half[2] = {(uint32_t)sees, (uint32_t)(sees >> 32)};
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[t][r] = half[t] >> (8 * (r / 4) + r % 4) & 1 ? s[t][r] : -INFINITY;
-        }
-        float most = s[0][0];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[t][r]);
-        most *= factor;
-        if (__ballot(most > top + 8.0f)) {                   // (the maximum moves only where a block beats it by more than 8)
-            most = fmaxf(top, fmaxf(most, __shfl_xor(most, 32, 64)));
-            const float by = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - most);
-            top = most;
-            sum *= by;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[t][r] *= by;
-        }
-        const float from = top == -INFINITY ? 0.0f : top;
-        bf16x8 w[4];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                u32x4 y;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 8 * j + 2 * e;
-                    const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], factor, -from));
-                    const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r + 1], factor, -from));
-                    sum += a + b;
-                    y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+                    for (int e = 0; e < 8; ++e)
+                        dot = __builtin_fmaf(half_of(x[e / 2], e % 2), half_of(y[e / 2], e % 2), dot);
                 }
-                w[2 * t + j] = __builtin_bit_cast(bf16x8, y);
-            }
+                dot += __shfl_xor(dot, 32, 64);
+                const bool sees = (u < limit) & (u >= lower);
+                const float score = sees ? dot * factor : -INFINITY, most = fmaxf(top, score);
+                const float by = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - most);
+                const float weight = __builtin_amdgcn_exp2f(score - (most == -INFINITY ? 0.0f : most));
+                top = most;
+                sum = sum * by + (h == 0 ? weight : 0.0f);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(block, i, t), w[i], o[t], 0, 0, 0);
-    };
-    // notes an infinite or NaN value in a block that not all rows see whole
-    const auto look = [&](const char* block) {
-        bool odd = false;
+                    for (int a = 0; a < 4; ++a) {
+                        const int e0 = 32 * t + 8 * a + 4 * h;
+                        const uint2 y = *reinterpret_cast<const uint2*>(vc + at + (e0 < head_dim ? e0 : 0));
 #pragma unroll
-        for (int i = 0; i < HALF / 4096; ++i) {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(block + HALF + i * 4096 + threadIdx.x * 16);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) odd |= not_finite(v[e]);
-        }
-        if (odd) tainted = 1;
-    };
-    if (threadIdx.x == 0) tainted = 0;                       // (before the first block's barrier)
-
-    // two buffers: block n+1 is on its way while block n is worked on; one barrier a block
-    if (step0 < step1) {
-        long long slot = slot_of(begin + step0 * kWideKeys + lane);
-        unsigned long long gone = __ballot(slot < 0), gone_next = 0;
-        stage(buf0, slot);
-        long long ahead = step0 + 1 < step1 ? slot_of(begin + (step0 + 1) * kWideKeys + lane) : -1;
-        const auto turn = [&](int step, char* now, char* next) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();                                 // block `step` is there, and nobody reads the other buffer any more
-            if (step + 1 < step1) {
-                gone_next = __ballot(ahead < 0);
-                stage(next, ahead);
-                if (step + 2 < step1) ahead = slot_of(begin + (step + 2) * kWideKeys + lane);
-            }
-            const int base = begin + step * kWideKeys;
-            if (!(base + kWideKeys <= block_limit && base >= block_lower)) look(now);
-            work(now, base, gone);
-            gone = gone_next;
-        };
-#pragma unroll 1
-        for (int step = step0; step < step1; step += 2) {
-            turn(step, buf0, buf1);
-            if (step + 1 < step1) turn(step + 1, buf1, buf0);
-        }
-    }
-
-    __syncthreads();
-    // An infinite or NaN value that some rows see and others do not: 0 times it is no 0.  Rare, and done over again key by key
-    // on the vector units, which leave out what a column does not see.
-    if (__builtin_amdgcn_readfirstlane(tainted)) {
-        asm volatile("" ::: "memory");                       // (keeps this path out of the common one)
-        top = -INFINITY;
-        sum = 0.0f;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
-        const int from = max(begin + step0 * kWideKeys, any_lower), to = min(begin + step1 * kWideKeys, any_limit);
-#pragma unroll 1
-        for (int u = from; u < to; ++u) {
-            const long long at = slot_of(u);
-            if (at < 0) continue;
-            float dot = 0.0f;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const int e0 = s * 16 + h * 8;
-                if (e0 >= p.head_dim) continue;
-                const u32x4 x = __builtin_bit_cast(u32x4, q[s]), y = *reinterpret_cast<const u32x4*>(kc + at + e0);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    dot = __builtin_fmaf(half_of(x[e / 2], e % 2), half_of(y[e / 2], e % 2), dot);
-            }
-            dot += __shfl_xor(dot, 32, 64);
-            const bool sees = (u < limit) & (u >= lower);
-            const float score = sees ? dot * factor : -INFINITY, most = fmaxf(top, score);
-            const float by = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - most);
-            const float weight = __builtin_amdgcn_exp2f(score - (most == -INFINITY ? 0.0f : most));
-            top = most;
-            sum = sum * by + (h == 0 ? weight : 0.0f);
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int a = 0; a < 4; ++a) {
-                    const int e0 = 32 * t + 8 * a + 4 * h;
-                    const uint2 y = *reinterpret_cast<const uint2*>(vc + at + (e0 < p.head_dim ? e0 : 0));
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const float v = half_of(b < 2 ? y.x : y.y, b % 2);
-                        o[t][4 * a + b] = o[t][4 * a + b] * by + (weight == 0.0f ? 0.0f : weight * v);
+                        for (int b = 0; b < 4; ++b) {
+                            const float v = half_of(b < 2 ? y.x : y.y, b % 2);
+                            o[t][4 * a + b] = o[t][4 * a + b] * by + (weight == 0.0f ? 0.0f : weight * v);
+                        }
                     }
-                }
-        }
-    }
+            }
+}
 
+// A wave's 32 columns into the workspace (parts) or the outputs; h, row, qh, is: this lane's half, row, query head and whether it has one.
+template <int DP>
+__device__ __forceinline__ void finish_wide(const ttf_attention_params& p, const Deal& d, const Sequence& seq, int head, int columns, int col,
+                                            int h, int row, long long qh, bool is, int target, float top, float sum, const f32x16 (&o)[DP / 32],
+                                            float* ws_out, float2* ws_stat)
+{
+    constexpr int NT = DP / 32;
     sum += __shfl_xor(sum, 32, 64);
     if (!is) return;
     if (d.parts > 1) {
         const int at = (d.slot + d.part) * p.kv_heads + head;
         if ((unsigned)at >= 2u * target) return;             // (cannot be with offsets that do not decrease)
-        const int part_row = at * kWideColumns + wave * 32 + m;
+        const int part_row = at * columns + col;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -320,15 +138,313 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
     if (p.lse && h == 0) p.lse[(long long)(seq.first + row) * p.heads + qh] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
 }
 
+template <int DP>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_attention_params p, ttf_kv_cache c, int target, float* ws_out,
+                                                                        float2* ws_stat, JoinNotes* notes)
+{
+    constexpr int PIECES = DP / 8, ROW = 2 * DP, HALF = kWideKeys * ROW;       // 16-byte pieces of a row; bytes of a row, of K's block
+    constexpr int CALLS = HALF / 4096, ROWS = 1024 / ROW;                      // loads of 1 KiB a wave makes for K, and for V; rows of one
+    constexpr int NT = DP / 32, KS = DP / 16;
+    __shared__ __attribute__((aligned(1024))) char buffer[4 * HALF];           // two of K and V
+    __shared__ int tainted;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, m = lane & 31;
+    const int head = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads;
+    Deal d;
+    if (!deal_out(p, c, kWideColumns, kWideKeys / 4, false, target, blockIdx.x, blockIdx.x == 0 ? notes : nullptr, d)) return;
+    const Sequence& seq = d.seq;
+    const int pairs = seq.rows * group;
+    // later rows see more keys: they go first
+    const int tile = tiles_of(seq.rows, group, kWideColumns) - 1 - d.tile, col0 = tile * kWideColumns;
+    d.slot += (tile - d.tile) * d.parts;
+    if (d.parts > 1 && d.part == 0 && head == 0 && threadIdx.x == 0 && d.note < target) notes->note[d.note] = JoinNote{d.b, tile, d.parts, d.slot};
+
+    const auto limit_of = [&](int row) { return p.causal ? (int)min((long long)seq.cached + row + 1, (long long)seq.length) : seq.length; };
+    const auto lower_of = [&](int row) {
+        return p.window > 0 ? (int)max(0ll, min((long long)seq.cached + row + 1 - p.window, 0x7fffffffll)) : 0;
+    };
+    // what all and what any of the workgroup's and of this wave's rows see
+    const int row_a = col0 / group, row_z = min(col0 + kWideColumns - 1, pairs - 1) / group;
+    const int begin0 = lower_of(row_a) & ~31, end = limit_of(row_z);
+    const int all = max(0, (int)(((long long)end - begin0 + kWideKeys - 1) / kWideKeys));
+    const int step0 = (int)((long long)all * d.part / d.parts), blocks = (int)((long long)all * (d.part + 1) / d.parts) - step0;
+    const int begin = begin0 + step0 * kWideKeys, stop = min(seq.length, begin + blocks * kWideKeys);
+
+    // Where the loads come from.  Lane l keeps the page number of page `window0` + l, read again when the blocks have passed it (a load
+    // whose result is needed in every block would be waited for together with all the younger ones, that go to LDS).  The block whose
+    // loads come next starts at entry `next_in` of page `next_page`.
+    const bf16_t *kc = (const bf16_t*)c.k + head * c.head_stride, *vc = (const bf16_t*)c.v + head * c.head_stride;
+    const int32_t* table = c.page_table + d.b * c.table_stride;
+    int next_page = (unsigned)begin / (unsigned)c.page_size, next_in = begin - next_page * c.page_size, next_base = begin;
+    int window0 = 0, window = -1;
+    bool holes = false;                                      // pages of the window that are not there
+    const auto open = [&](int page) {
+        window0 = page;
+        const bool there = (long long)(page + lane) * c.page_size < stop;
+        window = there ? table[page + lane] : -1;
+    };
+    const auto opened = [&] {
+        asm volatile("" : "+v"(window));                     // (waited for here)
+        holes = __ballot((window < 0 || window >= c.pages) && (long long)(window0 + lane) * c.page_size < stop) != 0;
+    };
+    open(next_page);
+
+    // this lane's column
+    const int pair = col0 + wave * 32 + m, row = pair / group;
+    const bool is = pair < pairs;
+    const int limit = is ? limit_of(row) : 0x7fffffff, lower = is ? lower_of(row) : 0;
+    const long long qh = (long long)head * group + pair % group;
+    u32x4 q_bits[KS];                                        // (on their way while the first keys and values are)
+    {
+        const bf16_t* from = (const bf16_t*)p.q + (seq.first + (is ? row : 0)) * p.q_row + qh * p.q_head;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int at = s * 16 + h * 8;
+            q_bits[s] = *reinterpret_cast<const u32x4*>(from + (at < p.head_dim ? at : 0));
+        }
+    }
+    const int wave0 = col0 + wave * 32, wave_row_z = min(wave0 + 31, pairs - 1) / group;
+    const bool wave_is = wave0 < pairs;
+    const int all_limit = limit_of(wave0 / group), any_limit = wave_is ? limit_of(wave_row_z) : 0;
+    const int all_lower = lower_of(wave_row_z), any_lower = lower_of(wave0 / group);
+    const int block_limit = limit_of(row_a), block_lower = lower_of(row_z);    // what all rows of the workgroup see
+
+    const auto slot_of = [&](int u) -> long long {           // element offset of entry u's slot, -1 where there is none
+        if (u >= seq.length) return -1;
+        const unsigned at = (unsigned)u / (unsigned)c.page_size;
+        const int page = table[at];
+        return page >= 0 && page < c.pages ? page * c.page_stride + (u - (int)at * c.page_size) * c.slot_stride : -1;
+    };
+    // Loads of a block, call i of this wave the KiB 4 i + wave: ROWS neighbouring rows.  Where these lie in one page (pages of whole
+    // ROWS slots), are all there and the head fills the row, their address is one for the wave and the lanes' part of it a constant.
+    unsigned lane_bytes[CALLS];
+    const bool plain = c.page_size % ROWS == 0 && p.head_dim == DP && c.slot_stride < (1ll << 24);
+#pragma unroll
+    for (int i = 0; i < CALLS; ++i) {
+        const int piece = (4 * i + wave) * 64 + lane, r = piece / PIECES;
+        lane_bytes[i] = (unsigned)(r % ROWS) * (unsigned)c.slot_stride * 2 + (piece % PIECES ^ swizzle<DP>(r)) * 16;
+    }
+    // The next block's sources: a lane's addresses in K, and which lanes read keys and values (the others: zeros).
+    unsigned long long source[CALLS], reads[CALLS];
+    const long long k_to_v = (const char*)vc - (const char*)kc;
+    const auto aim = [&] {
+        const int last = next_in + kWideKeys - 1;
+        int pages_on = 0, in_last = last;                    // pages that the block reaches beyond its first
+        while (in_last >= c.page_size) {
+            in_last -= c.page_size;
+            ++pages_on;
+        }
+        if (next_page + pages_on >= window0 + 64) {
+            open(next_page);
+            opened();
+        }
+        if (plain && next_base + kWideKeys <= stop && !holes) {
+            int page = next_page, in = next_in + ROWS * wave;
+#pragma unroll
+            for (int i = 0; i < CALLS; ++i) {
+                while (in >= c.page_size) {
+                    in -= c.page_size;
+                    ++page;
+                }
+                source[i] = (unsigned long long)kc + 2 * (__builtin_amdgcn_readlane(window, page - window0) * c.page_stride + in * c.slot_stride) +
+                            lane_bytes[i];
+                reads[i] = ~0ull;
+                in += 4 * ROWS;
+            }
+        } else {
+            const long long slot = next_base + lane < stop ? slot_of(next_base + lane) : -1;
+#pragma unroll
+            for (int i = 0; i < CALLS; ++i) {
+                const int piece = (4 * i + wave) * 64 + lane, r = piece / PIECES, e = (piece % PIECES ^ swizzle<DP>(r)) * 8;
+                const long long at = __shfl(slot, r, 64);
+                const bool there = at >= 0 && e < p.head_dim;
+                source[i] = there ? (unsigned long long)(kc + at + e) : (unsigned long long)&kZeros;
+                reads[i] = __ballot(there);
+            }
+        }
+        next_base += kWideKeys;
+        next_page += pages_on;
+        next_in = in_last + 1;
+        if (next_in == c.page_size) {
+            next_in = 0;
+            ++next_page;
+        }
+    };
+
+    // load n of the 2 CALLS of a block: of K, then of V
+    const auto load = [&](int n, int to) {
+        const int i = n % CALLS;
+        unsigned long long from = source[i];
+        if (n >= CALLS) from = reads[i] >> lane & 1 ? from + k_to_v : from;
+        load_to_lds(from, lds_offset(buffer) + to + n / CALLS * HALF + (4 * i + wave) * 1024);
+    };
+
+    const float factor = p.scale == 0.0f ? 1.0f : fabsf(p.scale) * kLog2e;
+    float top = -INFINITY, sum = 0.0f;
+    f32x16 o[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+
+    // A lane's places in a block.  The pieces' swap is an XOR of bits inside a row, so the place of another piece is an XOR with a
+    // constant, another row's an offset.  They are worked out anew every block (`hide`): kept, they would take 16 registers.
+    const int vr = (lane & 15) >> 2, low = (lane >> 4 & 1) * 2 + ((lane & 3) >> 1);
+    const int v_place = HALF + (4 * h + vr) * ROW + (DP == 64 ? vr >> 1 : vr) * 64 + (low ^ h) * 16 + (lane & 1) * 8;
+    const int k_place = m * ROW + (h ^ swizzle<DP>(m)) * 16;
+    const auto hide = [](int at) {
+        asm volatile("" : "+v"(at));
+        return at;
+    };
+
+    bf16x8 q[KS];
+    // Block at place `at` of the buffer.  The next block's loads are spread over its first products: issued all at once they hold
+    // up the waves until the last is taken (2000 rows over 31k keys: 728 us, spread out ... us).
+    const auto work = [&](int at, int to, int base, bool gaps) {
+        const int kp = hide(k_place + at), vp = hide(v_place + at);
+        f32x16 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(buffer + (kp ^ (i * 32)) + 32 * t * ROW), q[i],
+                                                               s[t], 0, 0, 0);
+                if (t == 1 && i < 2 * CALLS) load(i, to);
+            }
+        static_assert(KS == 2 * CALLS, "a load for every pair of products");
+        if (!(base + kWideKeys <= all_limit && base >= all_lower && !gaps)) {
+            // bit k: this column sees the block's key k + 4 h
+            const unsigned long long gone = gaps ? __ballot(slot_of(base + lane) < 0) : 0ull;
+            const int from = min(max(lower - base, 0), 64), to = min(max(limit - base, 0), 64);
+            const unsigned long long below = to == 64 ? ~0ull : (1ull << to) - 1, above = from == 64 ? 0ull : ~0ull << from;
+            const unsigned long long sees = (below & above & ~gone) >> (4 * h);
+            const uint32_t half[2] = {(uint32_t)sees, (uint32_t)(sees >> 32)};
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[t][r] = half[t] >> (8 * (r / 4) + r % 4) & 1 ? s[t][r] : -INFINITY;
+        }
+        // The weights against the maximum so far; where they get large, or there is none, against the block's own over again.
+        bf16x8 w[4];
+        float added;
+        bool last = false;
+        for (;;) {
+            const float from = top == -INFINITY ? 0.0f : top;
+            float part[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                u32x4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 8 * (i % 2) + 2 * e;
+                    const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][r], factor, -from));
+                    const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][r + 1], factor, -from));
+                    part[0] += a;
+                    part[1] += b;
+                    y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+                }
+                w[i] = __builtin_bit_cast(bf16x8, y);
+            }
+            added = part[0] + part[1];
+            if (last || !__ballot(!(added <= 256.0f) | (top == -INFINITY))) break;
+            float most = s[0][0];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) most = fmaxf(most, s[t][r]);
+            most = fmaxf(most, __shfl_xor(most, 32, 64)) * factor;
+            most = fmaxf(top, most);
+            const float by = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - most);
+            top = most;
+            sum *= by;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[t][r] *= by;
+            last = true;
+        }
+        sum += added;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                s16x4 part[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds_s16x4*)((lds_char*)buffer + (vp ^ (t * 64 + j * 32)) + (16 * i + 8 * j) * ROW));
+                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7)), w[i], o[t], 0, 0, 0);
+            }
+    };
+    // notes an infinite or NaN value in a block that not all rows see whole
+    const auto look = [&](const char* block) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < HALF / 4096; ++i) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(block + HALF + i * 4096 + threadIdx.x * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd |= not_finite(v[e]);
+        }
+        if (odd) tainted = 1;
+    };
+    if (threadIdx.x == 0) tainted = 0;                       // (before the first block's barrier)
+
+    // two buffers: block j + 1 is on its way while block j is worked on; one barrier a block
+    if (blocks > 0) {
+        opened();
+        aim();
+        bool gaps = holes;
+#pragma unroll
+        for (int n = 0; n < 2 * CALLS; ++n) load(n, 0);
+        const uint32_t flip = p.scale < 0.0f ? 0x80008000u : 0u, keep = p.scale == 0.0f ? 0u : ~0u;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+            q[s] = __builtin_bit_cast(bf16x8, is && s * 16 + h * 8 < p.head_dim ? (q_bits[s] ^ flip) & keep : u32x4{0, 0, 0, 0});
+#pragma unroll 1
+        for (int j = 0; j < blocks; ++j) {
+            const int at = j % 2 * 2 * HALF, base = begin + j * kWideKeys;
+            wait_for_loads();
+            __syncthreads();                                 // block j is there, and nobody reads the other buffer any more
+            const bool now = gaps;
+            aim();                                           // (past the last block: zeros)
+            gaps = holes;
+            if (!(base + kWideKeys <= block_limit && base >= block_lower)) look(buffer + at);
+            if (base < any_limit && base + kWideKeys > any_lower) {
+                work(at, 2 * HALF - at, base, now);
+            } else {
+#pragma unroll
+                for (int n = 0; n < 2 * CALLS; ++n) load(n, 2 * HALF - at);
+            }
+        }
+        wait_for_loads();                                 // (no load to LDS outlives the wave)
+    }
+
+    __syncthreads();
+    // An infinite or NaN value that some rows see and others do not: 0 times it is no 0.  Rare, and done over again key by key
+    // on the vector units, which leave out what a column does not see.
+    if (__builtin_amdgcn_readfirstlane(tainted)) {
+        asm volatile("" ::: "memory");                       // (keeps this path out of the common one)
+        const int from = max(begin, any_lower), to = min(begin + blocks * kWideKeys, any_limit);
+        by_keys<DP>(p.head_dim, kc, vc, slot_of, from, to, limit, lower, factor, q, top, sum, o);
+    }
+    finish_wide<DP>(p, d, seq, head, kWideColumns, wave * 32 + m, h, row, qh, is, target, top, sum, o, ws_out, ws_stat);
+}
+
 }  // namespace
 
 hipError_t launch_attention_wide(const ttf_attention_params& p, const ttf_kv_cache& c, int width, int target, unsigned grid, float* ws_out,
                                  float2* ws_stat, JoinNotes* notes, hipStream_t s)
 {
-    if (width == 64) k_attend_wide<64><<<grid, 256, 0, s>>>(p, c, target, ws_out, ws_stat, notes);
-    else if (width == 128) k_attend_wide<128><<<grid, 256, 0, s>>>(p, c, target, ws_out, ws_stat, notes);
-    else k_attend_wide<256><<<grid, 256, 0, s>>>(p, c, target, ws_out, ws_stat, notes);
-    return hipGetLastError();
+    const auto go = [&](auto kernel) {
+        kernel<<<grid, 256, 0, s>>>(p, c, target, ws_out, ws_stat, notes);
+        return hipGetLastError();
+    };
+    return width == 64 ? go(k_attend_wide<64>) : width == 128 ? go(k_attend_wide<128>) : go(k_attend_wide<256>);
 }
 
 }  // namespace ttf
