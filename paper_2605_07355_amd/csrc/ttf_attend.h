@@ -37,7 +37,7 @@ __device__ __forceinline__ Sequence sequence_of(const ttf_attention_params& p, c
 // one key head, or (`neighbours`, where there is enough work) each walk along the same blocks for a key head of its own: then
 // the workgroup reads four neighbouring heads of a slot, 1 KiB where one head is 256 bytes, which the memory likes better.  Every tile of a
 // sequence is cut into the same number of parts along the context, so many that no part is longer than `per` turns, where all parts
-// together are about `target` workgroups (a power of two).
+// together are about `target` workgroups (a power of two; `even`: a little less than it or than twice as many).
 //   part id -> key head (four of them) fastest, then part, then tile, then sequence.
 // Tiles of more than one part leave (maximum, sum, unnormalised row) of each part and head in the workspace, and part 0 a note for
 // the join.  With n key heads a workgroup, those rows' tiles are at most 2 n target (parts of cut tiles are more than per / 2 turns long
@@ -70,9 +70,38 @@ __device__ __forceinline__ int tiles_of(int rows, int group, int columns)
     return (int)((unsigned)(rows * group + columns - 1) / (unsigned)columns);    // (rows * heads <= 2^27)
 }
 
+// Turns a part at most, so that the workgroups come out in whole rounds of `target`: one that runs alone at the end costs as much as a full
+// round of them.  64 lengths are tried, a lane each, from half of an even `share` on, for the least sum of the rounds' longest parts and
+// what a part costs besides (kPartTurns: its start, and its rows to the workspace and back; 5 and 14 choose alike).  At most 2 target
+// workgroups, or the share stays.  `tiles` and `turns`: of sequence `lane`, at most 64 of them.
+//   2000 rows over 31k keys 600 -> 512 us, 300 over 100k 361 -> 268 us, 4 x 128 rows over 8k keys 80 -> 64 us, 20 rows 37.1 -> 38.2 us
+constexpr float kPartTurns = 9.0f;
+__device__ inline int even_turns(int batch, int kv_heads, int target, double share, int per, int tiles, int turns)
+{
+    const int lane = threadIdx.x & 63;
+    if (__ballot(turns >= 1 << 18) || wave_sum((float)tiles) * kv_heads > 2.0f * target) return per;    // (past it the quotients below may be off)
+    const double aim = share * 0.5 * (1.0 + lane / 16.0);
+    const int mine = aim < 1.0 ? 1 : (int)__builtin_ceil(aim);
+    const float inverse = 1.0f / mine * (1.0f - 0x1p-21f);   // n / mine, rounded up: 1 / n at least above a whole number, or that number
+    float all = 0.0f, most = 0.0f;
+    for (int b = 0; b < batch; ++b) {
+        const float n = (float)__builtin_amdgcn_readlane(turns, b), parts = fmaxf(1.0f, __builtin_ceilf(n * inverse));
+        const float many = (float)__builtin_amdgcn_readlane(tiles, b);
+        all += many * parts;
+        if (many > 0.0f) most = fmaxf(most, n / parts);
+    }
+    all *= kv_heads;
+    const float cost = all <= 2.0f * target ? __builtin_ceilf(all / target) * (most + kPartTurns) : INFINITY;
+    float least = cost;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) least = fminf(least, __shfl_xor(least, d, 64));
+    const unsigned long long best = __ballot(cost == least);
+    return least == INFINITY || !best ? per : __builtin_amdgcn_readlane(mine, __ffsll(best) - 1);
+}
+
 // The deal of workgroup `block`.  Every wave works it out by itself from the lengths, 64 sequences at a time (batches of up to 64
 // read them once).  False where nothing is left for it.  With `notes`, counts the tiles of more than one part as well.
-__device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cache& c, int columns, int keys, bool neighbours, int target,
+__device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cache& c, int columns, int keys, bool neighbours, bool even, int target,
                                 int block, JoinNotes* notes, Deal& d)
 {
     const int lane = threadIdx.x & 63, group = p.heads / p.kv_heads;
@@ -93,9 +122,10 @@ __device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cach
     }
     // a part of `per` turns: per blocks of one wave and four heads, or 4 per blocks of four waves and one head
     const double share = __builtin_ceil(total * p.kv_heads / (4.0 * target));
-    const int per = __builtin_amdgcn_readfirstlane(share < 1.0 ? 1 : share > 1e9 ? 1000000000 : (int)share);
+    int per = __builtin_amdgcn_readfirstlane(share < 1.0 ? 1 : share > 1e9 ? 1000000000 : (int)share);
+    if (even && p.batch <= 64) per = even_turns(p.batch, p.kv_heads, target, total * p.kv_heads / (4.0 * target), per, tiles, (blocks + 3) >> 2);
     d.heads = neighbours && per >= kNeighbourTurns ? kNeighbours : 1;
-    const int waves = 4 / d.heads, unit = block / (p.kv_heads / d.heads);
+    const int waves = 4 / d.heads, unit = __builtin_amdgcn_readfirstlane(block / (p.kv_heads / d.heads));
     int units = 0, slots = 0, split = 0;
     bool found = false;
     for (int i = 0; i < p.batch; i += 64) {
@@ -112,7 +142,7 @@ __device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cach
             d.parts = of(parts);
             const int in = unit - of(upto - mine);
             if ((unsigned)in >= (unsigned)of(mine)) return false;    // (sums past 32 bits: offsets that make no sense)
-            d.tile = in / d.parts;
+            d.tile = __builtin_amdgcn_readfirstlane(in / d.parts);      // (a division leaves it in a vector register)
             d.part = in - d.tile * d.parts;
             d.slot = of(slots_upto - held) + d.tile * d.parts;
             d.note = of(split_upto - notes_held) + d.tile;

@@ -14,6 +14,7 @@
 // permutes; product i then holds the entries d = NI c + i, c = 0..15.  So neither K nor V goes through LDS.
 //
 // Few rows are bound by the bytes of the cache: 16 KiB of K and V a wave in flight while the block before is worked on.
+#include <algorithm>
 #include <type_traits>
 
 #include "ttf_attend.h"
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, m = lane & 15;
     const int group = p.heads / p.kv_heads;
     Deal d;
-    if (!deal_out(p, c, columns, KB, neighbours, target, blockIdx.x, blockIdx.x == 0 ? notes : nullptr, d)) return;
+    if (!deal_out(p, c, columns, KB, neighbours, false, target, blockIdx.x, blockIdx.x == 0 ? notes : nullptr, d)) return;
     const int first_head = blockIdx.x % (p.kv_heads / d.heads) * d.heads, waves = 4 / d.heads;    // `waves` share a head
     const int head = first_head + (d.heads > 1 ? wave : 0), turn = d.heads > 1 ? 0 : wave;
     const Sequence& seq = d.seq;
@@ -517,7 +518,7 @@ Choice choose(const ttf_attention_params& p)
     x.wide = p.dtype == TTF_BF16 && pairs > 32;
     if (x.wide) {
         x.columns = 128;
-        x.target = 512;
+        x.target = x.width == 256 ? 256 : 512;               // (one and two workgroups a CU)
         x.slots = 2 * x.target;
         return x;
     }
@@ -606,7 +607,7 @@ hipError_t launch_attention(const ttf_attention_params& p, const ttf_kv_cache& c
         if (x.width == 128) return few(type, std::integral_constant<int, 128>());
         return few(type, std::integral_constant<int, 256>());
     };
-    const hipError_t e = x.wide ? launch_attention_wide(p, c, x.width, x.target, most_tiles(p, x) * p.kv_heads + x.target, w.out, w.stat, w.notes, s)
+    const hipError_t e = x.wide ? launch_attention_wide(p, c, x.width, x.target, std::max(2u * x.target, most_tiles(p, x) * p.kv_heads + x.target), w.out, w.stat, w.notes, s)
                        : p.dtype == TTF_BF16 ? of_width(bf16_t{}) : of_width(float{});
     if (e != hipSuccess) return e;
     return p.dtype == TTF_BF16 ? launch_join<bf16_t>(p, x, w, s) : launch_join<float>(p, x, w, s);

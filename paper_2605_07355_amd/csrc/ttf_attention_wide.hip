@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, m = lane & 31;
     const int head = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads;
     Deal d;
-    if (!deal_out(p, c, kWideColumns, kWideKeys / 4, false, target, blockIdx.x, blockIdx.x == 0 ? notes : nullptr, d)) return;
+    if (!deal_out(p, c, kWideColumns, kWideKeys / 4, false, true, target, blockIdx.x, blockIdx.x == 0 ? notes : nullptr, d)) return;
     const Sequence& seq = d.seq;
     const int pairs = seq.rows * group;
     // later rows see more keys: they go first
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
 
     bf16x8 q[KS];
     // Block at place `at` of the buffer.  The next block's loads are spread over its first products: issued all at once they hold
-    // up the waves until the last is taken (2000 rows over 31k keys: 728 us, spread out ... us).
+    // up the waves until the last is taken (2000 rows over 31k keys: 728 us, spread out 598 us, before the parts came in whole rounds).
     const auto work = [&](int at, int to, int base, bool gaps) {
         const int kp = hide(k_place + at), vp = hide(v_place + at);
         f32x16 s[2];

@@ -256,6 +256,17 @@ def test_attention(rows, cached, heads, kv_heads, D, page, dtype, causal, window
     _check_attention(out, lse, q, ks, vs, rows, cached, causal, window, dtype)
 
 
+@pytest.mark.parametrize("rows,cached,heads,D", [
+    ([33, 0, 35, 40], [5000, 3, 5900, 6200], 64, 64),        # two rounds of parts
+    ([34, 36, 33], [6100, 5500, 5800], 32, 256),
+    ([34] + 69 * [1], [3000] + 69 * [20], 4, 128),           # more sequences than lanes
+])
+def test_attention_of_rows_in_many_parts(rows, cached, heads, D):
+    q, k, v, table, ks, vs = _problem(rows, cached, heads, heads, D, 16, BF, slack_rows=1)
+    out, lse = _run_attention(q, k, v, table, rows, cached, max_rows=max(rows))
+    _check_attention(out, lse, q, ks, vs, rows, cached, True, 0, BF)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("max_rows", [1, 4, 8, 100, 1 << 20])
 def test_attention_does_not_rely_on_max_rows(dtype, max_rows):
