@@ -436,30 +436,34 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
 }
 
 // Joins the parts of a tile: out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s, in the order of the parts.  Workgroups go by
-// the notes that the parts' kernel left; a wave takes `each` columns, one after the other.
+// the notes that the parts' kernel left.  A wave takes `each` columns, one after the other, or where each is 0 a workgroup one column, a
+// quarter of the parts a wave.
 template <typename T, int EACH>
 __global__ __launch_bounds__(256) void k_attend_join(ttf_attention_params p, int columns, int each, int slots,
                                                      const float* __restrict__ ws_out, const float2* __restrict__ ws_stat,
                                                      const JoinNotes* __restrict__ notes)
 {
     constexpr int DP = 64 * EACH, AHEAD = 8;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads;
-    const int n = blockIdx.x / p.kv_heads;
+    __shared__ float quarter[4][EACH + 2][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = p.heads / p.kv_heads;
+    const int head = blockIdx.x % p.kv_heads, n = blockIdx.x / p.kv_heads;
     const JoinNote d = notes->note[n];
     if (n >= notes->count) return;                           // (what the note holds was not written by this call)
     if ((unsigned)((d.slot + d.parts - 1) * p.kv_heads + head) >= (unsigned)slots) return;
     const int2 rows = rows_of(p.row_offsets, d.b, p.rows);
-    for (int x = 0; x < each; ++x) {
-        const int col = (blockIdx.y * 4 + wave) * each + x, pair = d.tile * columns + col;
+    const int q = each ? d.parts : (max(4 * AHEAD, d.parts) + 4 * AHEAD - 1) / (4 * AHEAD) * AHEAD;    // parts a wave, whole batches
+    const int from = each ? 0 : min(wave * q, d.parts), to = min(from + q, d.parts);
+    for (int x = 0; x < max(each, 1); ++x) {
+        const int col = each ? (blockIdx.y * 4 + wave) * each + x : blockIdx.y, pair = d.tile * columns + col;
         if (col >= columns || pair >= rows.y * group) return;
         const auto at = [&](int part) { return ((d.slot + part) * p.kv_heads + head) * columns + col; };
         float most = -INFINITY;
-        for (int s = lane; s < d.parts; s += 64) most = fmaxf(most, ws_stat[at(s)].x);
+        for (int s = from + lane; s < to; s += 64) most = fmaxf(most, ws_stat[at(s)].x);
 #pragma unroll
         for (int y = 1; y < 64; y <<= 1) most = fmaxf(most, __shfl_xor(most, y, 64));
         float l = 0.0f, v[EACH] = {};
-        for (int s0 = 0; s0 < d.parts; s0 += 64) {
-            const int parts = min(64, d.parts - s0);
+        for (int s0 = from; s0 < to; s0 += 64) {
+            const int parts = min(64, to - s0);
             float by = 0.0f;
             if (lane < parts) {
                 const float2 t = ws_stat[at(s0 + lane)];
@@ -481,14 +485,36 @@ __global__ __launch_bounds__(256) void k_attend_join(ttf_attention_params p, int
             }
         }
         l = wave_sum(l);
+        if (!each && d.parts > AHEAD) {                      // the quarters, in their order
+            quarter[wave][EACH][lane] = most;
+            quarter[wave][EACH + 1][lane] = l;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) quarter[wave][i][lane] = v[i];
+            __syncthreads();
+            l = 0.0f;
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, quarter[w][EACH][lane]);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) v[i] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float m = quarter[w][EACH][lane], by = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+                l += by * quarter[w][EACH + 1][lane];
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) v[i] += by == 0.0f ? 0.0f : by * quarter[w][i][lane];
+            }
+            most = top;
+        }
+        if (!each && wave > 0) return;
         const int row = rows.x + pair / group, h = head * group + pair % group;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        T* to = (T*)p.out + row * p.o_row + h * p.o_head + lane * EACH;
+        T* to_row = (T*)p.out + row * p.o_row + h * p.o_head + lane * EACH;
         if (lane * EACH < p.head_dim) {
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
-                if constexpr (sizeof(T) == 2) to[i].bits = __builtin_bit_cast(uint16_t, (__bf16)(v[i] * inv));
-                else to[i] = v[i] * inv;
+                if constexpr (sizeof(T) == 2) to_row[i].bits = __builtin_bit_cast(uint16_t, (__bf16)(v[i] * inv));
+                else to_row[i] = v[i] * inv;
             }
         }
         if (p.lse && lane == 0) p.lse[(long long)row * p.heads + h] = l == 0.0f ? -INFINITY : most * kLn2 + logf(l);
@@ -522,7 +548,7 @@ Choice choose(const ttf_attention_params& p)
         x.slots = 2 * x.target;
         return x;
     }
-    x.tiles = pairs <= 16 ? 1 : (pairs <= 32 || p.dtype == TTF_BF16) ? 2 : 4;
+    x.tiles = pairs <= 16 ? 1 : (pairs <= 32 || p.dtype == TTF_BF16 || x.width > 64) ? 2 : 4;    // (fp32 of 128 entries: four spill, 20 x 29 rows over 14k keys 945 us, two 779)
     if (x.width == 256 && p.dtype == TTF_F32) x.tiles = 1;
     x.columns = pairs < 16 * x.tiles ? (int)pairs : 16 * x.tiles;    // no more than there are: the parts' rows take that much less room
     x.neighbours = p.kv_heads % kNeighbours == 0;
@@ -569,10 +595,11 @@ hipError_t launch(const ttf_attention_params& p, const ttf_kv_cache& c, const Ch
 template <typename T>
 hipError_t launch_join(const ttf_attention_params& p, const Choice& x, const Parts& w, hipStream_t s)
 {
-    // A wave to a column; four to a wave of the many columns of wide tiles, few of which are cut into parts as a rule.
-    const int each = x.wide ? 4 : 1;
+    // Few columns: a workgroup to each.  More: a wave to each.  Many tiles, few of which are cut as a rule: up to four to a wave (20 rows
+    // over 8192 entries 38.4 us with four, 33.0 with two, 30.8 with one; 8 clips of up to 1000 rows 61.1, 61.2, 63.4 us).
     const unsigned tiles = most_tiles(p, x) * p.kv_heads;
-    const dim3 grid(tiles < (unsigned)x.slots / 2 ? tiles : (unsigned)x.slots / 2, (unsigned)((x.columns + 4 * each - 1) / (4 * each)));
+    const int each = x.columns <= 16 ? 0 : tiles <= 256 ? 1 : tiles <= 512 ? 2 : 4;
+    const dim3 grid(tiles < (unsigned)x.slots / 2 ? tiles : (unsigned)x.slots / 2, (unsigned)(each ? (x.columns + 4 * each - 1) / (4 * each) : x.columns));
     const auto go = [&](auto kernel) {
         kernel<<<grid, 256, 0, s>>>(p, x.columns, each, x.slots, w.out, w.stat, w.notes);
         return hipGetLastError();
@@ -599,7 +626,7 @@ hipError_t launch_attention(const ttf_attention_params& p, const ttf_kv_cache& c
         if constexpr (sizeof(T) == 2 || DP < 256) {
             if (x.tiles == 2) return launch<T, DP, 2>(p, c, x, w, s);
         }
-        if constexpr (sizeof(T) == 4 && DP < 256) return launch<T, DP, 4>(p, c, x, w, s);
+        if constexpr (sizeof(T) == 4 && DP == 64) return launch<T, DP, 4>(p, c, x, w, s);
         return hipErrorInvalidValue;                         // (choose() names no other)
     };
     const auto of_width = [&](auto type) {
