@@ -49,6 +49,13 @@ struct Deal {
     int note;              // its number among the tiles of more than one part
     Sequence seq;
 };
+// Whether no tile is cut into parts, and none joined, because the table has no room for a long context: up to 512 entries, 256 in fp32 (8 clips
+// of up to 200 rows 31.6 -> 16.3 us, 64 tokens over up to 400 entries 27.2 -> 23.7; fp32, 10 x 15 rows over 200 29.8 -> 23.4, but one token
+// over 400 20 -> 38).
+__host__ __device__ inline bool uncut(const ttf_attention_params& p, const ttf_kv_cache& c)
+{
+    return (long long)c.page_size * c.table_width <= (p.dtype == TTF_BF16 ? 512 : 256);
+}
 constexpr int kNeighbours = 4, kNeighbourTurns = 8;          // least turns a part that make it worth it
 struct JoinNote { int b, tile, parts, slot; };
 struct JoinNotes { int count, pad[3]; JoinNote note[1]; };
@@ -129,6 +136,7 @@ __device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cach
     if (even && p.batch <= 64) per = even_turns(p.batch, p.kv_heads, target, share, per, tiles, (blocks + 3) >> 2);
     d.heads = neighbours && per >= kNeighbourTurns ? kNeighbours : 1;
     const int waves = 4 / d.heads, unit = __builtin_amdgcn_readfirstlane(block / (p.kv_heads / d.heads));
+    const bool whole = uncut(p, c);
     int units = 0, slots = 0, split = 0;
     bool found = false;
     for (int i = 0; i < p.batch; i += 64) {
@@ -137,7 +145,7 @@ __device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cach
         // One column's parts are joined one after the other: of a long context they get longer with its root (one token over 16796 entries
         // of two key heads 24.2 -> 18.3 us, over 10^6 of one 235 -> 121 us, with the join in quarters)
         const int least = even ? per : max(per, (int)__builtin_amdgcn_sqrtf(0.03f * turns));
-        const int parts = max(1, (int)((unsigned)(turns + least - 1) / (unsigned)least)), mine = tiles * parts;
+        const int parts = whole || turns == 0 ? 1 : (int)((unsigned)(turns + least - 1) / (unsigned)least), mine = tiles * parts;
         const int upto = units + wave_prefix(mine), held = parts > 1 ? mine : 0, notes_held = parts > 1 ? tiles : 0;
         const int slots_upto = slots + wave_prefix(held), split_upto = split + wave_prefix(notes_held);
         const unsigned long long after = __ballot(upto > unit);

@@ -637,6 +637,7 @@ hipError_t launch_attention(const ttf_attention_params& p, const ttf_kv_cache& c
     const hipError_t e = x.wide ? launch_attention_wide(p, c, x.width, x.target, std::max(2u * x.target, most_tiles(p, x) * p.kv_heads + x.target), w.out, w.stat, w.notes, s)
                        : p.dtype == TTF_BF16 ? of_width(bf16_t{}) : of_width(float{});
     if (e != hipSuccess) return e;
+    if (uncut(p, c)) return hipSuccess;
     return p.dtype == TTF_BF16 ? launch_join<bf16_t>(p, x, w, s) : launch_join<float>(p, x, w, s);
 }
 
