@@ -49,12 +49,14 @@ struct Deal {
     int note;              // its number among the tiles of more than one part
     Sequence seq;
 };
-// Whether no tile is cut into parts, and none joined, because the table has no room for a long context: up to 512 entries, 256 in fp32 (8 clips
+// Whether no tile is cut into parts, and none joined, because table or window leave no long context: up to 512 entries, 256 in fp32 (8 clips
 // of up to 200 rows 31.6 -> 16.3 us, 64 tokens over up to 400 entries 27.2 -> 23.7; fp32, 10 x 15 rows over 200 29.8 -> 23.4, but one token
 // over 400 20 -> 38).
 __host__ __device__ inline bool uncut(const ttf_attention_params& p, const ttf_kv_cache& c)
 {
-    return (long long)c.page_size * c.table_width <= (p.dtype == TTF_BF16 ? 512 : 256);
+    const long long room = (long long)c.page_size * c.table_width;
+    const long long reach = p.window > 0 ? (long long)p.window + p.rows : room;    // (a sequence has at most all the rows)
+    return (room < reach ? room : reach) <= (p.dtype == TTF_BF16 ? 512 : 256);
 }
 constexpr int kNeighbours = 4, kNeighbourTurns = 8;          // least turns a part that make it worth it
 struct JoinNote { int b, tile, parts, slot; };
