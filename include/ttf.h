@@ -388,7 +388,7 @@ typedef struct {
     const int32_t* row_offsets;                     /* [batch+1]                                       */
     const int32_t* cached;                          /* [batch] entries in the cache before these rows  */
     const void* q;                                  /* [rows, heads, D] by the strides                 */
-    void* out;                                      /* [rows, heads, D] by the strides; may be q       */
+    void* out;                                      /* [rows, heads, D] by the strides; may be q itself, same strides */
     float* lse;                                     /* optional [rows, heads]                          */
     int64_t q_row, q_head, o_row, o_head;
 } ttf_attention_params;

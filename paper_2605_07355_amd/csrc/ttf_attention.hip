@@ -449,8 +449,10 @@ __global__ __launch_bounds__(256) void k_attend_join(ttf_attention_params p, int
     const int head = blockIdx.x % p.kv_heads, n = blockIdx.x / p.kv_heads;
     const JoinNote d = notes->note[n];
     if (n >= notes->count) return;                           // (what the note holds was not written by this call)
-    if ((unsigned)((d.slot + d.parts - 1) * p.kv_heads + head) >= (unsigned)slots) return;
+    // (with offsets that decrease, workgroups past the grid have left theirs unwritten: any bits)
+    if ((unsigned)d.b >= (unsigned)p.batch || d.slot < 0 || d.parts < 1 || ((long long)d.slot + d.parts) * p.kv_heads > slots) return;
     const int2 rows = rows_of(p.row_offsets, d.b, p.rows);
+    if ((unsigned)d.tile >= (unsigned)tiles_of(rows.y, group, columns)) return;
     const int q = each ? d.parts : (max(4 * AHEAD, d.parts) + 4 * AHEAD - 1) / (4 * AHEAD) * AHEAD;    // parts a wave, whole batches
     const int from = each ? 0 : min(wave * q, d.parts), to = min(from + q, d.parts);
     for (int x = 0; x < max(each, 1); ++x) {
@@ -540,7 +542,9 @@ Choice choose(const ttf_attention_params& p)
 {
     Choice x{};
     x.width = p.head_dim <= 64 ? 64 : p.head_dim <= 128 ? 128 : 256;
-    const long long pairs = (long long)(p.max_rows < p.rows ? p.max_rows : p.rows) * (p.heads / p.kv_heads);
+    // (max_rows below the mean would give tiles of few columns to many rows: a grid past what a launch may have)
+    const int mean = (int)(((long long)p.rows + p.batch - 1) / p.batch), most = p.max_rows < p.rows ? p.max_rows : p.rows;
+    const long long pairs = (long long)(most > mean ? most : mean) * (p.heads / p.kv_heads);
     x.wide = p.dtype == TTF_BF16 && pairs > 32;
     if (x.wide) {
         x.columns = 128;

@@ -25,6 +25,12 @@ ttf_status check_rows(const void* p, int64_t row, int64_t head, int rows, int he
     return !aligned(p) || row % unit != 0 || head % unit != 0 ? TTF_ERR_UNSUPPORTED : TTF_OK;
 }
 
+// Whether an output that is the input itself has other strides than it.
+bool crossed(const void* from, int64_t row, int64_t head, const void* to, int64_t to_row, int64_t to_head, int rows, int heads)
+{
+    return from == to && ((rows > 1 && row != to_row) || (heads > 1 && head != to_head));
+}
+
 // Sizes that every launch grid and every 32-bit index of the kernels has room for.
 bool sizes_fit(int rows, int batch, int heads, int kv_heads)
 {
@@ -64,12 +70,15 @@ ttf_status check_qk(const ttf_qk_params* p, bool append)
     if (st == TTF_OK && p->heads > 0) {
         st = check_rows(p->q, p->q_row, p->q_head, p->rows, p->heads, p->head_dim, p->dtype);
         if (st == TTF_OK) st = check_rows(p->q_out, p->qo_row, p->qo_head, p->rows, p->heads, p->head_dim, p->dtype);
+        if (st == TTF_OK && crossed(p->q, p->q_row, p->q_head, p->q_out, p->qo_row, p->qo_head, p->rows, p->heads)) st = TTF_ERR_INVALID_ARG;
     }
     if (st == TTF_OK && p->kv_heads > 0) {
         st = check_rows(p->k, p->k_row, p->k_head, p->rows, p->kv_heads, p->head_dim, p->dtype);
         if (st == TTF_OK)
             st = append ? check_rows(p->v, p->v_row, p->v_head, p->rows, p->kv_heads, p->head_dim, p->dtype)
                         : check_rows(p->k_out, p->ko_row, p->ko_head, p->rows, p->kv_heads, p->head_dim, p->dtype);
+        if (st == TTF_OK && !append && crossed(p->k, p->k_row, p->k_head, p->k_out, p->ko_row, p->ko_head, p->rows, p->kv_heads))
+            st = TTF_ERR_INVALID_ARG;
     }
     if (st == TTF_OK && (!aligned(p->q_weight) || !aligned(p->k_weight))) st = TTF_ERR_UNSUPPORTED;
     return st;
@@ -184,6 +193,7 @@ ttf_status ttf_paged_attention(const ttf_attention_params* params, const ttf_kv_
     if (!p.row_offsets || !p.cached || !workspace) return TTF_ERR_INVALID_ARG;
     st = check_rows(p.q, p.q_row, p.q_head, p.rows, p.heads, p.head_dim, p.dtype);
     if (st == TTF_OK) st = check_rows(p.out, p.o_row, p.o_head, p.rows, p.heads, p.head_dim, p.dtype);
+    if (st == TTF_OK && crossed(p.q, p.q_row, p.q_head, p.out, p.o_row, p.o_head, p.rows, p.heads)) st = TTF_ERR_INVALID_ARG;
     if (st == TTF_OK) st = check_cache(cache, p.kv_heads, p.head_dim, p.dtype);
     if (st != TTF_OK) return st;
     if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return TTF_ERR_UNSUPPORTED;

@@ -292,6 +292,31 @@ def test_attention_without_some_pages(rows, page):
     assert bool((lse[rows[0]:] == -math.inf).all())
 
 
+@pytest.mark.parametrize("heads,rows,max_rows", [(4, 40, 1), (4, 8, 8), (32, 60, 60)])
+def test_offsets_that_decrease_stay_inside_the_buffers(heads, rows, max_rows):
+    """More work than the grid holds, and notes of every kind in the workspace: the rows past `rows` and the guards stay."""
+    import paper_2605_07355_amd as ttf
+    batch, D, length = 40, 64, 4000
+    g = _gen(3)
+    table, pages = _table([rows], [length], 16, g)
+    k, v = _cache(pages, 16, 4, D, BF, False, fill=0.5)
+    table = table.repeat(batch, 1)
+    offsets = torch.tensor([0 if b % 2 == 0 else rows for b in range(batch + 1)]).int()
+    cached = torch.full((batch,), 10).int()
+    cached[batch - 2:] = length
+    cache = ttf.TTFKVCache(k.cuda(), v.cuda(), table.cuda())
+    need = ttf.ttf_attention_workspace_size(rows, batch, heads, 4, D, max_rows=max_rows)
+    for fill in (0, 1, 0x7f, 0x80, 0xff):
+        buffer = torch.full((rows + 64, heads, D), 5.0, dtype=BF, device="cuda")
+        lse = torch.full((rows + 64, heads), 5.0, device="cuda")
+        ttf.ttf_paged_attention(torch.ones((rows, heads, D), dtype=BF, device="cuda"), cache, offsets.cuda(), cached.cuda(),
+                                max_rows=max_rows, out=buffer[32:32 + rows], lse=lse[32:32 + rows],
+                                workspace=torch.full((need + 256,), fill, dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        for x in (buffer, lse):
+            assert bool((x[:32] == 5.0).all()) and bool((x[32 + rows:] == 5.0).all())
+
+
 def test_attention_of_short_tables_and_odd_lengths():
     """Entries beyond the table are not there; a negative length sees nothing."""
     rows, cached = [2, 3, 1], [40, 20, 0]

@@ -105,6 +105,27 @@ def test_null_structures_and_workspace():
                 assert ttf.ttf_attention_workspace_size(rows, 1, 8, 2, D, dtype) <= 512 << 20
 
 
+@pytest.mark.parametrize("change", [dict(qo_row=512), dict(qo_head=256, qo_row=64), dict(ko_row=256)])
+def test_outputs_over_their_inputs_keep_the_strides(change):
+    assert serving._library().ttf_qk_norm_rope(ctypes.byref(_qk(**change)), None) == INVALID
+    if "ko_row" not in change:                               # (an append writes no k_out)
+        assert serving._library().ttf_cache_append(ctypes.byref(_qk(**change)), ctypes.byref(_cache()), None) == INVALID
+
+
+@pytest.mark.parametrize("change", [dict(o_row=512), dict(o_head=256, o_row=64)])
+def test_attention_over_its_queries_keeps_the_strides(change):
+    p = _attention(**change)
+    assert serving._library().ttf_paged_attention(ctypes.byref(p), ctypes.byref(_cache()), A, 1 << 40, None) == INVALID
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,batch", [(1 << 24, 1), (1 << 24, 1000), (100, 2)])
+def test_max_rows_below_the_mean_counts_as_the_mean(rows, batch, dtype):
+    mean = -(-rows // batch)
+    size = [ttf.ttf_attention_workspace_size(rows, batch, 4, 4, 64, dtype, max_rows=n) for n in (1, mean)]
+    assert size[0] == size[1]
+
+
 def test_binding_refuses():
     x = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
     with pytest.raises(ValueError):                       # no CPU path
