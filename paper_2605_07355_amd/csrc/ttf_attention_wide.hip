@@ -300,21 +300,36 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
     bf16x8 q[KS];
     // Block at place `at` of the buffer.  The next block's loads are spread over its first products: issued all at once they hold
     // up the waves until the last is taken (2000 rows over 31k keys: 728 us, spread out 598 us, before the parts came in whole rounds).
+    // Of a SIMD's two waves the one that multiplies goes first, the other takes its weights in between (8 clips of up to 3600 rows 407 -> 384 us,
+    // the other way round 392; with one wave a SIMD it only costs).
+    const auto first = [&](bool it) {
+        if constexpr (DP == 256) return;
+        if (it) __builtin_amdgcn_s_setprio(1);
+        else __builtin_amdgcn_s_setprio(0);
+    };
+    // Operands are read from LDS four products with K, three with V ahead (the same clips 403 -> 381 us, heads of 256 entries 1160 -> 980 us against
+    // the compiler's own order).
     const auto work = [&](int at, int to, int base, bool gaps) {
         const int kp = hide(k_place + at), vp = hide(v_place + at);
+        first(true);
         f32x16 s[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+        const auto k_frag = [&](int n) { return *reinterpret_cast<const bf16x8*>(buffer + (kp ^ (n / 2 * 32)) + 32 * (n % 2) * ROW); };
+        constexpr int KA = 4, VA = 3;
+        bf16x8 k[KA];
 #pragma unroll
-        for (int i = 0; i < KS; ++i)
+        for (int n = 0; n < KA; ++n) k[n] = k_frag(n);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(buffer + (kp ^ (i * 32)) + 32 * t * ROW), q[i],
-                                                               s[t], 0, 0, 0);
-                if (t == 1 && i < 2 * CALLS) load(i, to);
-            }
+        for (int n = 0; n < 2 * KS; ++n) {
+            __builtin_amdgcn_sched_barrier(0);
+            s[n % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[n % KA], q[n / 2], s[n % 2], 0, 0, 0);
+            if (n + KA < 2 * KS) k[n % KA] = k_frag(n + KA);
+            if (n % 2 == 1) load(n / 2, to);
+        }
+        first(false);
         static_assert(KS == 2 * CALLS, "a load for every pair of products");
         if (!(base + kWideKeys <= all_limit && base >= all_lower && !gaps)) {
             // bit k: this column sees the block's key k + 4 h
@@ -368,18 +383,25 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
             last = true;
         }
         sum += added;
+        first(true);
+        const auto v_frag = [&](int n) {
+            s16x4 part[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int j = 0; j < 2; ++j)
+                part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_s16x4*)((lds_char*)buffer + (vp ^ (n % NT * 64 + j * 32)) + (16 * (n / NT) + 8 * j) * ROW));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        bf16x8 v[VA];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                s16x4 part[2];
+        for (int n = 0; n < VA; ++n) v[n] = v_frag(n);
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_s16x4*)((lds_char*)buffer + (vp ^ (t * 64 + j * 32)) + (16 * i + 8 * j) * ROW));
-                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7)), w[i], o[t], 0, 0, 0);
-            }
+        for (int n = 0; n < 4 * NT; ++n) {
+            __builtin_amdgcn_sched_barrier(0);
+            o[n % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[n % VA], w[n / NT], o[n % NT], 0, 0, 0);
+            if (n + VA < 4 * NT) v[n % VA] = v_frag(n + VA);
+        }
+        first(false);
     };
     // notes an infinite or NaN value in a block that not all rows see whole
     const auto look = [&](const char* block) {
