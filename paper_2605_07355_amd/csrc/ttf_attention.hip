@@ -438,12 +438,13 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
 // Joins the parts of a tile: out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s, in the order of the parts.  Workgroups go by
 // the notes that the parts' kernel left.  A wave takes `each` columns, one after the other, or where each is 0 a workgroup one column, a
 // quarter of the parts a wave.
-template <typename T, int EACH>
+//   EACH  entries of a column a lane;  AHEAD  parts whose rows are on their way at once
+template <typename T, int EACH, int AHEAD>
 __global__ __launch_bounds__(256) void k_attend_join(ttf_attention_params p, int columns, int each, int slots,
                                                      const float* __restrict__ ws_out, const float2* __restrict__ ws_stat,
                                                      const JoinNotes* __restrict__ notes)
 {
-    constexpr int DP = 64 * EACH, AHEAD = 8;
+    constexpr int DP = 64 * EACH;
     __shared__ float quarter[4][EACH + 2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = p.heads / p.kv_heads;
     const int head = blockIdx.x % p.kv_heads, n = blockIdx.x / p.kv_heads;
@@ -608,7 +609,9 @@ hipError_t launch_join(const ttf_attention_params& p, const Choice& x, const Par
         kernel<<<grid, 256, 0, s>>>(p, x.columns, each, x.slots, w.out, w.stat, w.notes);
         return hipGetLastError();
     };
-    return x.width == 64 ? go(k_attend_join<T, 1>) : x.width == 128 ? go(k_attend_join<T, 2>) : go(k_attend_join<T, 4>);
+    // Where there are many tiles, each is in few parts (4 x 512 rows over 8192 entries, two to four: eight at once 25 us, four 22 us).
+    if (each > 1) return x.width == 64 ? go(k_attend_join<T, 1, 4>) : x.width == 128 ? go(k_attend_join<T, 2, 4>) : go(k_attend_join<T, 4, 4>);
+    return x.width == 64 ? go(k_attend_join<T, 1, 8>) : x.width == 128 ? go(k_attend_join<T, 2, 8>) : go(k_attend_join<T, 4, 8>);
 }
 
 }  // namespace
