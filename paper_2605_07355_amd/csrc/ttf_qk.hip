@@ -6,7 +6,7 @@
 // is formed in 64 bits (a position of 10^6 times a frequency of 1 has lost 2^-5 rad in 32), reduced to turns in [-1/2, 1/2] there, and
 // only then rounded for the sine and cosine, some 60 instructions.  A wave takes a row's share of the heads, forms every angle once, one a
 // lane, and hands them to its heads through LDS; 8 lanes then hold one head of 128, the two halves of every pair in the same lane.
-// Measured: 648 MB of 16 clips' queries and keys 118 us (5.5 TB/s), 778 MB appended 141 us (5.5 TB/s), fp32 103 MB 21 us (4.9 TB/s).
+// Measured: 648 MB of 16 clips' queries and keys 116 us (5.6 TB/s), 778 MB appended 139 us (5.6 TB/s), fp32 103 MB 20 us (5.1 TB/s).
 #include "ttf_device.h"
 #include "ttf_serve.h"
 
