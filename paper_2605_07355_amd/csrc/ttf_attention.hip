@@ -546,7 +546,9 @@ Choice choose(const ttf_attention_params& p)
     // (max_rows below the mean would give tiles of few columns to many rows: a grid past what a launch may have)
     const int mean = (int)(((long long)p.rows + p.batch - 1) / p.batch), most = p.max_rows < p.rows ? p.max_rows : p.rows;
     const long long pairs = (long long)(most > mean ? most : mean) * (p.heads / p.kv_heads);
-    x.wide = p.dtype == TTF_BF16 && pairs > 32;
+    // Between 17 and 32 columns either kernel may win with heads of up to 128 entries (32 x 8 rows over 8000 entries 124 us with few, 117 with many; 64 x 6 over
+    // 400 20 and 28); with 256 the one for few spills (475 and 370 us, 82 and 80).
+    x.wide = p.dtype == TTF_BF16 && pairs > (x.width == 256 ? 16 : 32);
     if (x.wide) {
         x.columns = 128;
         x.target = x.width == 256 ? 256 : 512;               // (one and two workgroups a CU)
@@ -630,7 +632,7 @@ hipError_t launch_attention(const ttf_attention_params& p, const ttf_kv_cache& c
         using T = decltype(type);
         constexpr int DP = decltype(width)::value;
         if (x.tiles == 1) return launch<T, DP, 1>(p, c, x, w, s);
-        if constexpr (sizeof(T) == 2 || DP < 256) {
+        if constexpr (DP < 256) {
             if (x.tiles == 2) return launch<T, DP, 2>(p, c, x, w, s);
         }
         if constexpr (sizeof(T) == 4 && DP == 64) return launch<T, DP, 4>(p, c, x, w, s);
