@@ -3,6 +3,7 @@
 #pragma once
 
 #include "ttf_device.h"
+#include "ttf_places.h"
 #include "ttf_serve.h"
 
 namespace ttf {

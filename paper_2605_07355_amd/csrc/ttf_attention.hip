@@ -146,7 +146,8 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
     };
     const char *kc = (const char*)((const T*)c.k + head * c.head_stride), *vc = (const char*)((const T*)c.v + head * c.head_stride);
     const unsigned slot_bytes = (unsigned)c.slot_stride * E;
-    const unsigned k_at = m * slot_bytes + 16 * g, v_at = 4 * g * slot_bytes + (!CUT || m * NI < p.head_dim ? m * NI * E : 0);
+    const int piece = CUT && DP == 64 ? first_piece(g, p.head_dim, E) : 16 * g;    // (longer ones have a first piece for every group)
+    const unsigned k_at = m * slot_bytes + piece, v_at = 4 * g * slot_bytes + (!CUT || m * NI < p.head_dim ? m * NI * E : 0);
 
     u32x4 k[TILES][KS];
     uint32_t v[4 * TILES][VW];
@@ -155,11 +156,11 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
         for (int t = 0; t < TILES; ++t) {
             const char* from;
             if constexpr (WHOLE) from = kc + max(0ll, x.tile[t]) * E + k_at;
-            else from = kc + max(0ll, __shfl(x.tile[0], 16 * t + m, 64)) * E + 16 * g;
+            else from = kc + max(0ll, __shfl(x.tile[0], 16 * t + m, 64)) * E + piece;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                k[t][s] = load_once<u32x4>(from + (CUT && (s * 64 + g * 16) / E >= p.head_dim ? 0 : s * 64));
-                if (CUT && (s * 64 + g * 16) / E >= p.head_dim) k[t][s] = u32x4{0, 0, 0, 0};
+                k[t][s] = load_once<u32x4>(from + (CUT ? next_piece(s, g, p.head_dim, E) : s * 64));
+                if (CUT && !has_piece(s, g, p.head_dim, E)) k[t][s] = u32x4{0, 0, 0, 0};
             }
         }
     };
