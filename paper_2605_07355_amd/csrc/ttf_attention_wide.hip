@@ -180,12 +180,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
     bool holes = false;                                      // pages of the window that are not there
     const auto open = [&](int page) {
         window0 = page;
-        const bool there = (long long)(page + lane) * c.page_size < stop;
-        window = there ? table[page + lane] : -1;
+        window = page_begins(page, lane, c.page_size, stop) ? table[page + lane] : -1;
     };
     const auto opened = [&] {
         asm volatile("" : "+v"(window));                     // (waited for here)
-        holes = __ballot((window < 0 || window >= c.pages) && (long long)(window0 + lane) * c.page_size < stop) != 0;
+        holes = __ballot((window < 0 || window >= c.pages) && page_begins(window0, lane, c.page_size, stop)) != 0;
     };
     open(next_page);
 

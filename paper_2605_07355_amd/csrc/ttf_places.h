@@ -10,4 +10,8 @@ constexpr int first_piece(int g, int head_dim, int entry_bytes) { return has_pie
 // How far from there its s-th is; where the head has none, the first again.
 constexpr int next_piece(int s, int g, int head_dim, int entry_bytes) { return has_piece(s, g, head_dim, entry_bytes) ? s * 64 : 0; }
 
+// Whether the lane-th page from `page` on, of page_size slots, begins before entry `stop`.  (Pages of one slot and a window over entries near 2^31:
+// the number is past 31 bits.)
+constexpr bool page_begins(int page, int lane, int page_size, int stop) { return (long long)((unsigned)page + (unsigned)lane) * page_size < stop; }
+
 }  // namespace ttf

@@ -31,3 +31,15 @@ def test_key_pieces_stay_inside_the_head(tmp_path, entry_bytes):
                 assert 0 <= at <= size - 16, (D, s, g)
                 if s * 64 + g * 16 < size:
                     assert at == s * 64 + g * 16
+
+
+def test_pages_are_looked_up_before_the_end_alone(tmp_path):
+    """Also where a window over entries near 2^31 begins at a page whose number, with a lane's, is past 31 bits."""
+    most = 2 ** 31 - 1
+    cases = [(first // size, size, stop) for size in (1, 2, 7, 64, 1 << 20) for first in (0, 96, 5000, most - 31, most)
+             for stop in (0, 1, 100, 0x7ff00000)]
+    got = iter(_values(tmp_path, "for (int lane = 0; lane < 64; ++lane) {\n"
+                       + "\n".join(f"put(page_begins({page}, lane, {size}, {stop}));" for page, size, stop in cases) + "\n}"))
+    for lane in range(64):
+        for page, size, stop in cases:
+            assert next(got) == ((page + lane) * size < stop), (page, lane, size, stop)
