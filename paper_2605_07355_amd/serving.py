@@ -151,24 +151,47 @@ def ttf_rope_table(rotary_dim: int, base: float = 10000.0, scaling: str = "plain
 
 class TTFKVCache:
     """A paged cache: ``k`` and ``v`` [pages, page_size, kv_heads, head_dim] with contiguous heads and the same
-    strides (``transpose(1, 2)`` of a cache that keeps heads first is fine), ``page_table`` int32 [batch, width]."""
+    strides (``transpose(1, 2)`` of a cache that keeps heads first is fine), ``page_table`` int32 [batch, width].
 
-    __slots__ = ("k", "v", "page_table", "_struct", "_batch", "_heads", "_head_dim", "_gpu")
+    What the tensors hold may change between calls.  ``page_table`` may be set to another tensor (a wider one, or
+    one of another batch), which the next call uses; other ``k`` and ``v`` are another cache.  Their addresses and
+    sizes are taken down here: none of them may be resized in place."""
+
+    __slots__ = ("_k", "_v", "_page_table", "_struct", "_batch", "_heads", "_head_dim", "_gpu")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor):
         shape, strides, gpu = k.shape, k.stride(), k.get_device()
         if len(shape) != 4 or shape != v.shape or strides != v.stride() or k.dtype is not v.dtype or strides[3] != 1:
             raise ValueError("k and v must be [pages, page_size, kv_heads, head_dim] with contiguous heads, alike in every way")
+        if gpu != v.get_device():
+            raise ValueError("k, v and page_table must live on one device")
+        self._k, self._v, self._gpu = k, v, gpu
+        self._heads, self._head_dim = shape[2], shape[3]
+        self.page_table = page_table
+
+    @property
+    def k(self) -> torch.Tensor:
+        return self._k
+
+    @property
+    def v(self) -> torch.Tensor:
+        return self._v
+
+    @property
+    def page_table(self) -> torch.Tensor:
+        return self._page_table
+
+    @page_table.setter
+    def page_table(self, page_table: torch.Tensor) -> None:
         if page_table.dim() != 2 or page_table.dtype is not torch.int32 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
             raise ValueError("page_table must be int32 [batch, width] with contiguous rows")
-        if not gpu == v.get_device() == page_table.get_device():
+        if page_table.get_device() != self._gpu:
             raise ValueError("k, v and page_table must live on one device")
-        self.k, self.v, self.page_table = k, v, page_table
-        pages, size, self._heads, self._head_dim = shape
-        self._batch, width = page_table.shape
-        self._gpu = gpu
-        self._struct = _pack_cache(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), strides[0], strides[1], strides[2],
-                                   page_table.stride(0) if self._batch > 1 else width, pages, size, width)
+        k, (batch, width) = self._k, page_table.shape
+        strides = k.stride()
+        self._struct = _pack_cache(k.data_ptr(), self._v.data_ptr(), page_table.data_ptr(), strides[0], strides[1], strides[2],
+                                   page_table.stride(0) if batch > 1 else width, k.shape[0], k.shape[1], width)
+        self._page_table, self._batch = page_table, batch
 
 
 _NONE = (0, 0, 0, 0)
@@ -250,7 +273,7 @@ def ttf_cache_append(cache: TTFKVCache, k: torch.Tensor, v: torch.Tensor, row_of
                      stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
     """Put normed and rotated keys and the values of packed rows into ``cache``: row i of sequence b becomes entry
     ``cached[b] + i``.  ``q`` is normed and rotated in the same launch.  Returns q_out (None without q)."""
-    if cache.k.dtype is not k.dtype or cache._gpu != k.get_device() or (cache._heads, cache._head_dim) != tuple(k.shape[1:]):
+    if cache._k.dtype is not k.dtype or cache._gpu != k.get_device() or (cache._heads, cache._head_dim) != tuple(k.shape[1:]):
         raise ValueError("the cache must have the heads, head_dim, dtype and device of k")
     if q is not None and q_out is None:
         q_out = _empty(q.shape, q.dtype, q.device, stream)
@@ -280,7 +303,7 @@ def ttf_paged_attention(q: torch.Tensor, cache: TTFKVCache, row_offsets: torch.T
     if q.dim() != 3:
         raise ValueError("q must be [rows, heads, head_dim]")
     (rows, heads, D), dtype, gpu = q.shape, q.dtype, q.get_device()
-    if cache.k.dtype is not dtype or cache._gpu != gpu or cache._head_dim != D:
+    if cache._k.dtype is not dtype or cache._gpu != gpu or cache._head_dim != D:
         raise ValueError("the cache must have the head_dim, dtype and device of q")
     if out is None:
         out = _empty((rows, heads, D), dtype, q.device, stream)

@@ -35,3 +35,23 @@ def test_windows_behind_the_end_of_the_table(rows, page, dtype):
             have = torch.full((len(rows),), cached, dtype=torch.int32, device="cuda")
             out = ttf.ttf_paged_attention(q, ttf.TTFKVCache(k, v, table), _offsets(rows).cuda(), have, window=window, lse=lse)
             assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+
+
+def test_a_cache_whose_page_table_grows():
+    """The table is replaced by a wider one between calls; the old one's memory holds other numbers by then."""
+    import paper_2605_07355_amd as ttf
+    rows, cached = [2, 1], [200, 77]
+    q, k, v, table, ks, vs = _problem(rows, cached, 4, 2, 64, 16, BF)
+    cache = ttf.TTFKVCache(k.cuda(), v.cuda(), table[:, :1].contiguous().cuda())
+    new = torch.randn((3, 2, 64), generator=torch.Generator().manual_seed(2)).to(BF)
+    old, cache.page_table = cache.page_table, table.cuda()
+    old.fill_(-1)
+    have, offsets = torch.tensor(cached).int().cuda(), _offsets(rows).cuda()
+    ttf.ttf_cache_append(cache, new.cuda(), new.cuda(), offsets, have)
+    first = 0
+    for b, (r, c) in enumerate(zip(rows, cached)):
+        ks[b][c:] = vs[b][c:] = new[first:first + r]
+        first += r
+    out, lse = torch.full_like(q, 5.0, device="cuda"), torch.full((3, 4), 5.0, device="cuda")
+    ttf.ttf_paged_attention(q.cuda(), cache, offsets, have, out=out, lse=lse)
+    _check_attention(out.cpu(), lse.cpu(), q, ks, vs, rows, cached, True, 0, BF)
