@@ -338,7 +338,8 @@ typedef struct {
  *   TTF_ROPE_BASE     base * factor^(R/(R-2)) in the place of base: the first pair stays, the last is divided by factor
  *   TTF_ROPE_PARTS    divided by factor to a share g_j in [0,1]: f (1 - g) + f / factor g, with g growing linearly in j from 0 to 1
  *                     between the pairs that turn `fast` and `slow` times over original_length positions (the first rounded
- *                     down, the second up, both kept within 0 .. R/2-1); attention_factor = 0.1 ln(factor) + 1
+ *                     down, the second up, neither below 0; beyond the last pair where all turn faster than that: the last is then
+ *                     divided in part, or not at all); attention_factor = 0.1 ln(factor) + 1
  *   TTF_ROPE_TURNS    the same with 1 - g linear in the number of turns between slow and fast; attention_factor = 1
  * and axis[j], the plane of each pair, from the number of pairs of every plane: sections[axes] (HOST; their sum is R/2; NULL: all
  * plane 0).  take_turns 0: one block of pairs after the other.  Otherwise the planes take turns: pair j goes to plane

@@ -134,8 +134,8 @@ ttf_status ttf_rope_table(int32_t rotary_dim, double base, int32_t scaling, doub
     const auto pair_of = [&](double n) { return rotary_dim * std::log(original_length / (n * two_pi)) / (2.0 * std::log(base)); };
     double low = 0.0, high = 0.0;
     if (scaling == TTF_ROPE_PARTS) {
-        low = std::fmin(std::fmax(std::floor(pair_of(fast)), 0.0), half - 1.0);
-        high = std::fmin(std::fmax(std::ceil(pair_of(slow)), 0.0), half - 1.0);
+        low = std::fmax(std::floor(pair_of(fast)), 0.0);
+        high = std::fmax(std::ceil(pair_of(slow)), 0.0);      // (beyond the last pair where that turns faster: no pair is divided whole)
     }
     for (int j = 0; j < half; ++j) {
         double f = std::pow(base, -2.0 * j / rotary_dim), g = 0.0;   // g: share that is divided

@@ -1,4 +1,6 @@
 """CPU-only checks of the entry points behind the compressed rows at the edges of what they accept."""
+import math
+
 import pytest
 import torch
 
@@ -22,3 +24,30 @@ def test_a_page_table_that_is_set_anew_is_the_one_used():
     for name in ("k", "v"):                                 # (their sizes and strides belong together)
         with pytest.raises(AttributeError):
             setattr(cache, name, k)
+
+
+@pytest.mark.parametrize("R,base,length,factor", [
+    (128, 1e4, 131072, 4.0),          # the last pair still turns twice
+    (64, 1e4, 131072, 8.0),
+    (128, 1e4, 4096, 16.0),           # the ramp ends between pairs
+    (64, 1e6, 32768, 4.0),
+    (16, 50.0, 100000, 4.0),          # all pairs turn more than 32 times: none is divided
+])
+def test_frequencies_divided_in_part_up_to_where_the_ramp_ends(R, base, length, factor):
+    fast, slow = 32.0, 1.0
+
+    def pair_that_turns(n):           # by bisection of the number of turns, which falls with the (broken) number of the pair
+        lo, hi = -1000.0, 1000.0
+        for _ in range(200):
+            mid = (lo + hi) / 2
+            lo, hi = (mid, hi) if length * base ** (-2 * mid / R) / (2 * math.pi) > n else (lo, mid)
+        return lo
+
+    low, high = max(0, math.floor(pair_that_turns(fast))), math.ceil(pair_that_turns(slow))
+    got = ttf.ttf_rope_table(R, base, scaling="parts", factor=factor, original_length=length, fast=fast, slow=slow, device="cpu")
+    f = [base ** (-2 * j / R) for j in range(R // 2)]
+    g = [min(max((j - low) / (high - low), 0.0), 1.0) for j in range(R // 2)]
+    want = torch.tensor([x * (1 - y) + x / factor * y for x, y in zip(f, g)], dtype=torch.float64)
+    assert torch.allclose(got.inv_freq, want, rtol=1e-13, atol=0)
+    if length * f[-1] / (2 * math.pi) > slow:              # a pair that turns more often than `slow` is not divided whole
+        assert got.inv_freq[-1] > f[-1] / factor * (1 + 1e-9)
