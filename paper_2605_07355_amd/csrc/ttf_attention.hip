@@ -540,13 +540,18 @@ struct Choice {
     int slots;      // tiles of parts that the workspace has room for
 };
 
-Choice choose(const ttf_attention_params& p)
+// Pairs of a row and a query head that the longest sequence brings to a key head.
+// (max_rows below the mean would give tiles of few columns to many rows: a grid past what a launch may have)
+long long pairs_of(const ttf_attention_params& p)
+{
+    const int mean = (int)(((long long)p.rows + p.batch - 1) / p.batch), most = p.max_rows < p.rows ? p.max_rows : p.rows;
+    return (long long)(most > mean ? most : mean) * (p.heads / p.kv_heads);
+}
+
+Choice choose(const ttf_attention_params& p, long long pairs)
 {
     Choice x{};
     x.width = p.head_dim <= 64 ? 64 : p.head_dim <= 128 ? 128 : 256;
-    // (max_rows below the mean would give tiles of few columns to many rows: a grid past what a launch may have)
-    const int mean = (int)(((long long)p.rows + p.batch - 1) / p.batch), most = p.max_rows < p.rows ? p.max_rows : p.rows;
-    const long long pairs = (long long)(most > mean ? most : mean) * (p.heads / p.kv_heads);
     // Between 17 and 32 columns either kernel may win with heads of up to 128 entries (32 x 8 rows over 8000 entries 124 us with few, 117 with many; 64 x 6 over
     // 400 20 and 28); with 256 the one for few spills (475 and 370 us, 82 and 80).
     x.wide = p.dtype == TTF_BF16 && pairs > (x.width == 256 ? 16 : 32);
@@ -619,15 +624,21 @@ hipError_t launch_join(const ttf_attention_params& p, const Choice& x, const Par
 
 }  // namespace
 
+size_t attention_workspace_used(const ttf_attention_params& p) { return carve_parts(choose(p, pairs_of(p)), nullptr).bytes; }
+
+// Fewer pairs may take more: the kernel for few rows has more workgroups.  With one kernel and number of column tiles the room
+// grows with the pairs, so it is greatest at the most pairs of one of them.
 size_t attention_workspace_bytes(const ttf_attention_params& p)
 {
-    const Choice x = choose(p);
-    return carve_parts(x, nullptr).bytes;
+    const long long pairs = pairs_of(p);
+    size_t most = 0;
+    for (const long long n : {pairs, 16ll, 32ll, 64ll}) most = std::max(most, carve_parts(choose(p, std::min(n, pairs)), nullptr).bytes);
+    return most;
 }
 
 hipError_t launch_attention(const ttf_attention_params& p, const ttf_kv_cache& c, void* workspace, hipStream_t s)
 {
-    const Choice x = choose(p);
+    const Choice x = choose(p, pairs_of(p));
     const Parts w = carve_parts(x, workspace);
     const auto few = [&](auto type, auto width) {
         using T = decltype(type);

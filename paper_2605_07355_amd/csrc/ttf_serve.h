@@ -16,7 +16,8 @@ void set_last_hip_error(hipError_t e);   // behind ttf_last_hip_error()
 
 hipError_t launch_qk(const ttf_qk_params& p, const ttf_kv_cache* cache, hipStream_t s);
 
-size_t attention_workspace_bytes(const ttf_attention_params& p);
+size_t attention_workspace_bytes(const ttf_attention_params& p);   // of this call and of every smaller one
+size_t attention_workspace_used(const ttf_attention_params& p);    // of this call
 hipError_t launch_attention(const ttf_attention_params& p, const ttf_kv_cache& c, void* workspace, hipStream_t s);
 
 // Rows of sequence b, clamped to the buffers: first row and number of rows (0 where the offsets make no sense).

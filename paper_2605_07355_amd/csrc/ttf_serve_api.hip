@@ -197,7 +197,7 @@ ttf_status ttf_paged_attention(const ttf_attention_params* params, const ttf_kv_
     if (st == TTF_OK) st = check_cache(cache, p.kv_heads, p.head_dim, p.dtype);
     if (st != TTF_OK) return st;
     if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return TTF_ERR_UNSUPPORTED;
-    if (workspace_bytes < attention_workspace_bytes(p)) return TTF_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < attention_workspace_used(p)) return TTF_ERR_WORKSPACE_TOO_SMALL;
     return done(launch_attention(p, *cache, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 

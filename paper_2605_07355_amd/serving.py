@@ -285,6 +285,8 @@ def ttf_cache_append(cache: TTFKVCache, k: torch.Tensor, v: torch.Tensor, row_of
 
 def ttf_attention_workspace_size(rows: int, batch: int, heads: int, kv_heads: int, head_dim: int,
                                  dtype: torch.dtype = torch.bfloat16, max_rows: Optional[int] = None) -> int:
+    """Bytes of workspace that ``ttf_paged_attention`` needs for such a call, and for every one with the same heads, head_dim and
+    dtype and no more rows, sequences and ``max_rows`` (default: all rows)."""
     p = _AttentionParams(_DTYPES[dtype], head_dim, heads, kv_heads, rows, batch, rows if max_rows is None else max_rows, 1, 0, 1.0)
     n = ctypes.c_size_t(0)
     _check(_library().ttf_attention_workspace_size(ctypes.byref(p), ctypes.byref(n)))
@@ -297,7 +299,8 @@ def ttf_paged_attention(q: torch.Tensor, cache: TTFKVCache, row_offsets: torch.T
                         workspace: Optional[torch.Tensor] = None,
                         stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Attention of the packed rows ``q`` [rows, heads, D] over ``cache``, whose sequences hold ``cached`` entries and these
-    rows' own (``ttf_cache_append`` first).  ``max_rows`` (most rows of one sequence; default: all) picks the kernel;
+    rows' own (``ttf_cache_append`` first).  ``max_rows`` (most rows of one sequence, at least 1; default: all) picks the kernel
+    and with it the room taken in ``workspace`` (uint8, of ttf_attention_workspace_size; taken from torch where not given);
     ``scale`` defaults to 1/sqrt(D); ``window`` > 0: a row looks back over that many entries, itself included; ``lse``
     float32 [rows, heads] is filled where given.  Rows outside ``row_offsets`` stay as they were."""
     if q.dim() != 3:

@@ -55,3 +55,15 @@ def test_a_cache_whose_page_table_grows():
     out, lse = torch.full_like(q, 5.0, device="cuda"), torch.full((3, 4), 5.0, device="cuda")
     ttf.ttf_paged_attention(q.cuda(), cache, offsets, have, out=out, lse=lse)
     _check_attention(out.cpu(), lse.cpu(), q, ks, vs, rows, cached, True, 0, BF)
+
+
+@pytest.mark.parametrize("heads,kv_heads,D,dtype", [(32, 8, 128, BF), (16, 4, 256, BF), (8, 4, 64, F32)])
+def test_one_workspace_for_a_large_chunk_and_then_small_ones(heads, kv_heads, D, dtype):
+    import paper_2605_07355_amd as ttf
+    work = torch.zeros(ttf.ttf_attention_workspace_size(600, 3, heads, kv_heads, D, dtype, max_rows=400), dtype=torch.uint8, device="cuda")
+    for rows, cached in (([400, 3, 197], [100, 3000, 20]), ([1, 1, 2], [900, 3000, 20]), ([1], [2500]), ([8, 5], [300, 1])):
+        q, k, v, table, ks, vs = _problem(rows, cached, heads, kv_heads, D, 16, dtype)
+        cache, have = ttf.TTFKVCache(k.cuda(), v.cuda(), table.cuda()), torch.tensor(cached).int().cuda()
+        out = ttf.ttf_paged_attention(q.cuda(), cache, _offsets(rows).cuda(), have, max_rows=max(rows), workspace=work)
+        own = ttf.ttf_paged_attention(q.cuda(), cache, _offsets(rows).cuda(), have, max_rows=max(rows))
+        assert torch.equal(out, own) and bool(torch.isfinite(out).all())

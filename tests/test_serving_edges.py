@@ -51,3 +51,20 @@ def test_frequencies_divided_in_part_up_to_where_the_ramp_ends(R, base, length, 
     assert torch.allclose(got.inv_freq, want, rtol=1e-13, atol=0)
     if length * f[-1] / (2 * math.pi) > slow:              # a pair that turns more often than `slow` is not divided whole
         assert got.inv_freq[-1] > f[-1] / factor * (1 + 1e-9)
+
+
+def test_a_workspace_is_enough_for_every_smaller_call():
+    """Sizes do not fall where rows, sequences or max_rows grow."""
+    counts = [1, 2, 3, 4, 5, 8, 9, 16, 17, 33, 64, 65, 500, 4096]
+    for dtype in (torch.bfloat16, torch.float32):
+        for heads, kv_heads, D in ((32, 8, 128), (16, 4, 256), (8, 8, 64), (7, 1, 72), (6, 2, 200), (64, 1, 64)):
+            size = lambda rows, batch, n: ttf.ttf_attention_workspace_size(rows, batch, heads, kv_heads, D, dtype, max_rows=n)  # noqa: E731
+            for rows in counts:
+                by_max = [size(rows, rows, n) for n in counts]
+                assert by_max == sorted(by_max), (dtype, heads, D, rows)
+            for n in counts:
+                by_rows = [size(rows, 4096, n) for rows in counts]
+                assert by_rows == sorted(by_rows), (dtype, heads, D, n)
+            # one sequence of all rows, and many that bring no more each
+            for n in counts:
+                assert size(n, 1, n) <= size(64 * n, 64, n)
