@@ -289,7 +289,8 @@ typedef enum { TTF_ROPE_HALF = 0, TTF_ROPE_INTERLEAVED = 1 } ttf_rope_layout;
 
 /*
  * Queries, keys and values of `rows` rows, with the norm and the rotation they get.  Strides are in elements; the
- * entries of a head are contiguous.  Pointers and strides of q, k, v and the outputs are multiples of 16 bytes.
+ * entries of a head are contiguous.  Pointers and strides of q, k, v and the outputs are multiples of 16 bytes; no two heads of an
+ * output share an entry.
  *
  *   norm     y_i = x_i w_i / sqrt(mean_i x_i^2 + eps) over the head_dim entries of a head, where the weight is given
  *   angle    theta_j = pos[axis[j]][row] * inv_freq[j] for the pairs j < rotary_dim / 2, formed in 64 bits
@@ -322,7 +323,7 @@ typedef struct {
 
 /* A paged cache: page p, slot s, head h of k (and of v) starts at element p*page_stride + s*slot_stride +
  * h*head_stride; entry t of sequence b is slot t % page_size of page page_table[b*table_stride + t / page_size].
- * Pointers and strides of k and v are multiples of 16 bytes. */
+ * Pointers and strides of k and v are multiples of 16 bytes; no two heads of a page share an entry where it is written. */
 typedef struct {
     void *k, *v;
     const int32_t* page_table;      /* [batch, table_width]                                     */

@@ -1,5 +1,6 @@
 // C ABI of the entry points behind the compressed rows: argument checks and the frequencies of a rotation.
 #include <cmath>
+#include <cstdlib>
 
 #include "ttf_serve.h"
 
@@ -15,7 +16,7 @@ ttf_status check_head(int dtype, int head_dim)
     return head_dim % 8 != 0 || head_dim > kMaxHeadDim ? TTF_ERR_UNSUPPORTED : TTF_OK;
 }
 
-// A [rows, heads, D] operand: strides that keep every head's rows apart, in steps of 16 bytes.
+// A [rows, heads, D] operand: strides in steps of 16 bytes, neighbouring rows and neighbouring heads apart.
 ttf_status check_rows(const void* p, int64_t row, int64_t head, int rows, int heads, int D, int dtype)
 {
     const int64_t unit = dtype == TTF_BF16 ? 8 : 4, most = 1ll << 40;
@@ -23,6 +24,17 @@ ttf_status check_rows(const void* p, int64_t row, int64_t head, int rows, int he
     if (row < 0 || head < 0 || row > most || head > most) return TTF_ERR_INVALID_ARG;
     if ((rows > 1 && row < D) || (heads > 1 && head < D)) return TTF_ERR_INVALID_ARG;
     return !aligned(p) || row % unit != 0 || head % unit != 0 ? TTF_ERR_UNSUPPORTED : TTF_OK;
+}
+
+// Whether two of the heads that are written share an entry: heads j apart in one direction and rows i in the other that meet.  (Strides as
+// check_rows leaves them: at least D where there are two.)
+bool folded(int64_t row, int64_t head, int rows, int heads, int D)
+{
+    if (rows < 2 || heads < 2 || row >= (heads - 1) * head + D || head >= (rows - 1) * row + D) return false;
+    for (int64_t j = 1; j < heads; ++j)
+        for (int64_t i = j * head / row, end = i + 1; i <= end && i < rows; ++i)
+            if (std::llabs(j * head - i * row) < D) return true;
+    return false;
 }
 
 // Whether an output that is the input itself has other strides than it.
@@ -71,13 +83,15 @@ ttf_status check_qk(const ttf_qk_params* p, bool append)
         st = check_rows(p->q, p->q_row, p->q_head, p->rows, p->heads, p->head_dim, p->dtype);
         if (st == TTF_OK) st = check_rows(p->q_out, p->qo_row, p->qo_head, p->rows, p->heads, p->head_dim, p->dtype);
         if (st == TTF_OK && crossed(p->q, p->q_row, p->q_head, p->q_out, p->qo_row, p->qo_head, p->rows, p->heads)) st = TTF_ERR_INVALID_ARG;
+        if (st == TTF_OK && folded(p->qo_row, p->qo_head, p->rows, p->heads, p->head_dim)) st = TTF_ERR_INVALID_ARG;
     }
     if (st == TTF_OK && p->kv_heads > 0) {
         st = check_rows(p->k, p->k_row, p->k_head, p->rows, p->kv_heads, p->head_dim, p->dtype);
         if (st == TTF_OK)
             st = append ? check_rows(p->v, p->v_row, p->v_head, p->rows, p->kv_heads, p->head_dim, p->dtype)
                         : check_rows(p->k_out, p->ko_row, p->ko_head, p->rows, p->kv_heads, p->head_dim, p->dtype);
-        if (st == TTF_OK && !append && crossed(p->k, p->k_row, p->k_head, p->k_out, p->ko_row, p->ko_head, p->rows, p->kv_heads))
+        if (st == TTF_OK && !append && (crossed(p->k, p->k_row, p->k_head, p->k_out, p->ko_row, p->ko_head, p->rows, p->kv_heads) ||
+                                        folded(p->ko_row, p->ko_head, p->rows, p->kv_heads, p->head_dim)))
             st = TTF_ERR_INVALID_ARG;
     }
     if (st == TTF_OK && (!aligned(p->q_weight) || !aligned(p->k_weight))) st = TTF_ERR_UNSUPPORTED;
@@ -171,6 +185,8 @@ ttf_status ttf_cache_append(const ttf_qk_params* params, const ttf_kv_cache* cac
 {
     ttf_status st = check_qk(params, true);
     if (st == TTF_OK) st = check_cache(cache, params->kv_heads, params->head_dim, params->dtype);
+    // (pages may share slots: which are written is the page table's to say)
+    if (st == TTF_OK && folded(cache->slot_stride, cache->head_stride, cache->page_size, params->kv_heads, params->head_dim)) st = TTF_ERR_INVALID_ARG;
     if (st != TTF_OK) return st;
     return done(launch_qk(*params, cache, static_cast<hipStream_t>(hip_stream)));
 }
@@ -194,6 +210,7 @@ ttf_status ttf_paged_attention(const ttf_attention_params* params, const ttf_kv_
     st = check_rows(p.q, p.q_row, p.q_head, p.rows, p.heads, p.head_dim, p.dtype);
     if (st == TTF_OK) st = check_rows(p.out, p.o_row, p.o_head, p.rows, p.heads, p.head_dim, p.dtype);
     if (st == TTF_OK && crossed(p.q, p.q_row, p.q_head, p.out, p.o_row, p.o_head, p.rows, p.heads)) st = TTF_ERR_INVALID_ARG;
+    if (st == TTF_OK && folded(p.o_row, p.o_head, p.rows, p.heads, p.head_dim)) st = TTF_ERR_INVALID_ARG;
     if (st == TTF_OK) st = check_cache(cache, p.kv_heads, p.head_dim, p.dtype);
     if (st != TTF_OK) return st;
     if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return TTF_ERR_UNSUPPORTED;

@@ -1,4 +1,5 @@
 """CPU-only checks of the entry points behind the compressed rows at the edges of what they accept."""
+import ctypes
 import math
 
 import pytest
@@ -6,6 +7,7 @@ import torch
 
 import paper_2605_07355_amd as ttf
 from paper_2605_07355_amd import serving
+from test_serving_checks import A, INVALID, SMALL, UNSUPPORTED, _attention, _cache, _qk
 
 
 def test_a_page_table_that_is_set_anew_is_the_one_used():
@@ -68,3 +70,40 @@ def test_a_workspace_is_enough_for_every_smaller_call():
             # one sequence of all rows, and many that bring no more each
             for n in counts:
                 assert size(n, 1, n) <= size(64 * n, 64, n)
+
+
+# strides of 8 rows and 4 heads (2 key heads) of 64 entries; whether two heads share an entry
+LAYOUTS = [(64, 64, True), (128, 64, True), (192, 64, True), (248, 64, True), (256, 64, False), (64, 504, True), (64, 512, False), (192, 128, True),
+           (320, 192, False), (1024, 600, False), (1024, 1088, False), (1024, 1080, True)]
+
+
+def _share(row, head, rows, heads, D):
+    at = [i * row + j * head for i in range(rows) for j in range(heads)]
+    return any(abs(a - b) < D for n, a in enumerate(at) for b in at[:n])
+
+
+@pytest.mark.parametrize("row,head,shares", LAYOUTS)
+def test_outputs_that_overlap_themselves_are_refused(row, head, shares):
+    """Every call ends in a refusal before any HIP call: INVALID for the layout, or what stands behind it."""
+    assert _share(row, head, 8, 4, 64) == shares
+    lib, other = serving._library(), 2 * A
+    # a misaligned norm weight and a workspace too small are found after the layouts
+    qk = dict(q_out=other, qo_row=row, qo_head=head, q_weight=A + 2)
+    want = INVALID if shares else UNSUPPORTED
+    assert lib.ttf_qk_norm_rope(ctypes.byref(_qk(**qk)), None) == want
+    assert lib.ttf_cache_append(ctypes.byref(_qk(**qk)), ctypes.byref(_cache()), None) == want
+    p = _attention(out=other, o_row=row, o_head=head)
+    assert lib.ttf_paged_attention(ctypes.byref(p), ctypes.byref(_cache()), A, 0, None) == (INVALID if shares else SMALL)
+    two = _share(row, head, 8, 2, 64)
+    assert lib.ttf_qk_norm_rope(ctypes.byref(_qk(k_out=other, ko_row=row, ko_head=head, q_weight=A + 2)), None) == (INVALID if two else UNSUPPORTED)
+    # inputs are only read
+    assert lib.ttf_qk_norm_rope(ctypes.byref(_qk(q_row=row, q_head=head, q_out=other, q_weight=A + 2)), None) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("slot,head", [(64, 64), (128, 64), (64, 960), (64, 1024), (192, 128), (320, 64)])
+def test_append_refuses_a_cache_whose_heads_overlap(slot, head):
+    lib, c = serving._library(), _cache(slot_stride=slot, head_stride=head)
+    if _share(slot, head, 16, 2, 64):
+        assert lib.ttf_cache_append(ctypes.byref(_qk()), ctypes.byref(c), None) == INVALID
+    # reading such a cache is harmless
+    assert lib.ttf_paged_attention(ctypes.byref(_attention()), ctypes.byref(c), A, 0, None) == SMALL
