@@ -368,7 +368,7 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
 #pragma unroll
                 for (int i = 0; i < NI; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) o[n][i][r] = o[n][i][r] * by + (weight == 0.0f ? 0.0f : weight * y[i][r]);
+                    for (int r = 0; r < 4; ++r) o[n][i][r] = o[n][i][r] * by + weight * y[i][r];
             }
         }
     }
@@ -412,7 +412,7 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
                 y[i] = 0.0f;
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
-                    y[i] += by[w] == 0.0f ? 0.0f : by[w] * lds[(w * 16 + col) * PAD + e0 + i];
+                    y[i] += d.heads == 1 || w == x ? by[w] * lds[(w * 16 + col) * PAD + e0 + i] : 0.0f;
             }
             if (d.parts > 1) {
                 const int at = (d.slot + d.part) * p.kv_heads + first_head + x;
@@ -436,7 +436,8 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
     }
 }
 
-// Joins the parts of a tile: out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s, in the order of the parts.  Workgroups go by
+// Joins the parts of a tile: out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s, in the order of the parts.  (A factor that underflows to 0
+// still multiplies its o: an infinite or NaN value that the row sees stays.)  Workgroups go by
 // the notes that the parts' kernel left.  A wave takes `each` columns, one after the other, or where each is 0 a workgroup one column, a
 // quarter of the parts a wave.
 //   EACH  entries of a column a lane;  AHEAD  parts whose rows are on their way at once
@@ -482,9 +483,9 @@ __global__ __launch_bounds__(256) void k_attend_join(ttf_attention_params p, int
                     for (int i = 0; i < EACH; ++i) y[s][i] = ws_out[(size_t)at(s0 + min(s1 + s, parts - 1)) * DP + lane * EACH + i];
 #pragma unroll
                 for (int s = 0; s < AHEAD; ++s) {
-                    const float w = s1 + s < parts ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, by), s1 + s)) : 0.0f;
+                    const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, by), s1 + s));
 #pragma unroll
-                    for (int i = 0; i < EACH; ++i) v[i] += w == 0.0f ? 0.0f : w * y[s][i];
+                    for (int i = 0; i < EACH; ++i) v[i] += s1 + s < parts ? w * y[s][i] : 0.0f;
                 }
             }
         }
@@ -506,7 +507,7 @@ __global__ __launch_bounds__(256) void k_attend_join(ttf_attention_params p, int
                 const float m = quarter[w][EACH][lane], by = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
                 l += by * quarter[w][EACH + 1][lane];
 #pragma unroll
-                for (int i = 0; i < EACH; ++i) v[i] += by == 0.0f ? 0.0f : by * quarter[w][i][lane];
+                for (int i = 0; i < EACH; ++i) v[i] += by * quarter[w][i][lane];
             }
             most = top;
         }

@@ -95,7 +95,7 @@ __device__ __forceinline__ void by_keys(int head_dim, const bf16_t* kc, const bf
 #pragma unroll
                         for (int b = 0; b < 4; ++b) {
                             const float v = half_of(b < 2 ? y.x : y.y, b % 2);
-                            o[t][4 * a + b] = o[t][4 * a + b] * by + (weight == 0.0f ? 0.0f : weight * v);
+                            o[t][4 * a + b] = o[t][4 * a + b] * by + (sees ? weight * v : 0.0f);
                         }
                     }
             }

@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+from serving_reference import attend, check, seen_mask
 from test_gpu_serving import BF, F32, _cache, _check_attention, _offsets, _problem, _run_attention
 
 pytestmark = pytest.mark.gpu
@@ -67,3 +68,39 @@ def test_one_workspace_for_a_large_chunk_and_then_small_ones(heads, kv_heads, D,
         out = ttf.ttf_paged_attention(q.cuda(), cache, _offsets(rows).cuda(), have, max_rows=max(rows), workspace=work)
         own = ttf.ttf_paged_attention(q.cuda(), cache, _offsets(rows).cuda(), have, max_rows=max(rows))
         assert torch.equal(out, own) and bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+@pytest.mark.parametrize("rows,cached,low,bad", [
+    ([1], [300], range(200), 40),              # not cut: waves join
+    ([1], [6000], range(5000), 70),            # cut into parts
+    ([20], [30], range(45), 40),               # seen from the middle of the chunk on
+    ([20], [30], range(36, 50), 40),
+    ([60, 1], [5000, 9], range(4000), 70),
+    ([200], [100], range(200), 150),
+    ([200], [100], range(101, 300), 150),
+])
+def test_a_value_of_tiny_weight_is_not_lost(rows, cached, low, bad, value, dtype):
+    """Weights of e^-512 are 0 in 32 bits; an infinite or NaN value that a row sees reaches it all the same."""
+    q, k, v, table, ks, vs = _problem(rows, cached, 4, 2, 64, 16, dtype, peak=0.05)
+    q[:, :, 0] = 16.0
+    for b, n in enumerate(r + c for r, c in zip(rows, cached)):
+        t = torch.arange(n)
+        ks[b][:, :, 0] = torch.where((t >= low.start) & (t < low.stop), -16.0, 16.0)[:, None].to(dtype)
+        if b == 0:
+            vs[b][bad, :, 7] = value
+        page = table[b].long()[t // 16]
+        k[page, t % 16], v[page, t % 16] = ks[b], vs[b]
+    out, lse = _run_attention(q, k, v, table, rows, cached, max_rows=max(rows), scale=1.0)
+    first = 0
+    for b, (r, c) in enumerate(zip(rows, cached)):
+        seen = seen_mask(r, c, r + c, True, 0, torch.ones(r + c, dtype=torch.bool))
+        for x in (range(r) if r < 30 else (0, 1, bad - c - 1, bad - c, r // 2, r - 1)):
+            if not 0 <= x < r:
+                continue
+            want, want_lse, slack, lse_slack = attend(q[first + x:first + x + 1], ks[b], vs[b], seen[x:x + 1], 1.0)
+            assert bool(torch.isfinite(want[..., 7]).all()) != bool(b == 0 and seen[x, bad])
+            check(out[first + x:first + x + 1], want, slack, dtype, f"row {x}")
+            check(lse[first + x:first + x + 1], want_lse, lse_slack, F32, "lse")
+        first += r
