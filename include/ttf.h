@@ -294,7 +294,8 @@ typedef enum { TTF_ROPE_HALF = 0, TTF_ROPE_INTERLEAVED = 1 } ttf_rope_layout;
  *
  *   norm     y_i = x_i w_i / sqrt(mean_i x_i^2 + eps) over the head_dim entries of a head, where the weight is given
  *   angle    theta_j = pos[axis[j]][row] * inv_freq[j] for the pairs j < rotary_dim / 2, formed in 64 bits
- *   rotate   (y_a, y_b) -> (y_a c - y_b s, y_b c + y_a s), c = attention_factor cos theta_j, s = attention_factor sin theta_j,
+ *   rotate   (y_a, y_b) -> (y_a c - y_b s, y_b c + y_a s), c = attention_factor cos theta_j, s = attention_factor sin theta_j, taken in 64
+ *            bits and rounded to 32 once,
  *            (a, b) = (j, j + rotary_dim/2) with TTF_ROPE_HALF, (2j, 2j+1) with TTF_ROPE_INTERLEAVED; entries from
  *            rotary_dim on are not rotated
  */

@@ -3,8 +3,9 @@
 //
 // A row's heads are independent and each entry is read and written once, so the bytes bound it: 2 T (Hq + Hk) D e, with the
 // values of an append 2 T (Hq + 2 Hk) D e.  What could cost more is the angles, D/2 a row: position times frequency
-// is formed in 64 bits (a position of 10^6 times a frequency of 1 has lost 2^-5 rad in 32), reduced to turns in [-1/2, 1/2] there, and
-// only then rounded for the sine and cosine, some 60 instructions.  A wave takes a row's share of the heads, forms every angle once, one a
+// is formed in 64 bits (a position of 10^6 times a frequency of 1 has lost 2^-5 rad in 32) and reduced to turns in [-1/2, 1/2] there; sine and
+// cosine are taken in 64 bits too and rounded once, since an angle rounded to 32 before errs by up to 2^-23.3 rad (16 clips 115.3 -> 116.1 us,
+// one token the same).  A wave takes a row's share of the heads, forms every angle once, one a
 // lane, and hands them to its heads through LDS; 8 lanes then hold one head of 128, the two halves of every pair in the same lane.
 // Measured: 648 MB of 16 clips' queries and keys 116 us (5.6 TB/s), 778 MB appended 139 us (5.6 TB/s), fp32 103 MB 20 us (5.1 TB/s).
 #include "ttf_device.h"
@@ -84,9 +85,9 @@ __global__ __launch_bounds__(256) void k_qk(ttf_qk_params p, ttf_kv_cache c, boo
         int a = p.axis ? p.axis[j] : 0;
         if (a < 0 || a >= p.axes) a = 0;
         const double turns = (double)p.pos[a * p.pos_stride + row] * (p.inv_freq[j] * 0.15915494309189533577);   // 1 / 2 pi
-        float s, co;
-        sincospif((float)(2.0 * (turns - __builtin_rint(turns))), &s, &co);
-        turn[wave][j] = float2{p.attention_factor * co, p.attention_factor * s};
+        double s, co;
+        sincospi(2.0 * (turns - __builtin_rint(turns)), &s, &co);
+        turn[wave][j] = float2{(float)(p.attention_factor * co), (float)(p.attention_factor * s)};
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();

@@ -104,3 +104,25 @@ def test_a_value_of_tiny_weight_is_not_lost(rows, cached, low, bad, value, dtype
             check(out[first + x:first + x + 1], want, slack, dtype, f"row {x}")
             check(lse[first + x:first + x + 1], want_lse, lse_slack, F32, "lse")
         first += r
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("factor", [1.0, 1.25])
+def test_sines_and_cosines_are_rounded_once(layout, factor):
+    """Pairs (1, 0) turn into (c, s): within half a step of fp32, and the error that the angle has in 64 bits."""
+    import paper_2605_07355_amd as ttf
+    rows, R = 4000, 128
+    g = torch.Generator().manual_seed(9)
+    pos = torch.randint(-(1 << 20), 1 << 20, (1, rows), generator=g).int()
+    freq = 10000.0 ** (-2.0 * torch.arange(R // 2).double() / R)
+    x = torch.zeros((rows, 1, R))
+    first, second = (slice(0, R // 2), slice(R // 2, R)) if layout == "half" else (slice(0, R, 2), slice(1, R, 2))
+    x[..., first] = 1.0
+    out, _ = ttf.ttf_qk_norm_rope(x.cuda(), None, pos.cuda(), ttf.TTFRope(freq.cuda(), layout=layout, attention_factor=factor))
+    out = out.cpu().double()
+    theta = pos[0].double()[:, None] * freq
+    # 64 bits: 1 / 2 pi, its product with the frequency, that with the position, each rounded, and sine and cosine themselves; here the product
+    slack = factor * 2.0 ** -53 * (4 * theta.abs() + 4)
+    for got, want in ((out[:, 0, first], factor * torch.cos(theta)), (out[:, 0, second], factor * torch.sin(theta))):
+        past = ((got - want).abs() - 2.0 ** -24 * (want.abs() + slack) - slack).max().item()
+        assert past <= 0
