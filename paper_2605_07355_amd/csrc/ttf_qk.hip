@@ -139,7 +139,26 @@ __global__ __launch_bounds__(256) void k_qk(ttf_qk_params p, ttf_kv_cache c, boo
             }
         }
         for (int m = 1; m < group; m <<= 1) squares += __shfl_xor(squares, m, 64);
-        const float scale = weight ? 1.0f / sqrtf(squares / (float)p.head_dim + p.eps) : 1.0f;
+        float mean = squares / (float)p.head_dim + p.eps;
+        // Squares that overflow, or are so small that they lose bits and eps does not cover them: the head over again, lifted by a power of two
+        // (below it all entries are below 2^-46, and 2^100 times as much has squares between 2^-98 and 2^116).  Rare, and the same for the head's lanes.
+        if (weight && !(mean >= 0x1p-100f && mean < INFINITY)) {
+            const float lift = mean < 0x1p-100f ? 0x1p100f : 0x1p-70f;
+            squares = 0.0f;
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) {
+                if (!to || sub + i * group >= units) continue;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    x[i][0][e] *= lift;
+                    x[i][1][e] *= lift;
+                    squares += x[i][0][e] * x[i][0][e] + x[i][1][e] * x[i][1][e];
+                }
+            }
+            for (int m = 1; m < group; m <<= 1) squares += __shfl_xor(squares, m, 64);
+            mean = squares / (float)p.head_dim + p.eps * lift * lift;
+        }
+        const float scale = weight ? 1.0f / sqrtf(mean) : 1.0f;
         if (!to) continue;
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {

@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from serving_reference import attend, check, seen_mask
+from serving_reference import attend, check, norm_rotate, seen_mask
 from test_gpu_serving import BF, F32, _cache, _check_attention, _offsets, _problem, _run_attention
 
 pytestmark = pytest.mark.gpu
@@ -126,3 +126,26 @@ def test_sines_and_cosines_are_rounded_once(layout, factor):
     for got, want in ((out[:, 0, first], factor * torch.cos(theta)), (out[:, 0, second], factor * torch.sin(theta))):
         past = ((got - want).abs() - 2.0 ** -24 * (want.abs() + slack) - slack).max().item()
         assert past <= 0
+
+
+@pytest.mark.parametrize("D,rot,layout", [(128, 128, "half"), (80, 32, "interleaved"), (72, 10, "half")])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_norms_of_heads_whose_squares_leave_the_range(D, rot, layout, dtype):
+    """Squares that overflow, or that all underflow where eps does not cover them, beside ordinary heads."""
+    import paper_2605_07355_amd as ttf
+    g = torch.Generator().manual_seed(D)
+    sizes = torch.tensor([1.0, 1e25, 1e-30, 3e36, 1e-37, 1e19, 1e-18, 1e18, 1e-20])
+    x = torch.randn((9, 3, D), generator=g) * sizes[:, None, None]
+    x[:, 1] = torch.randn((9, D), generator=g)              # the ordinary neighbour in each row
+    x[1, 2, 1:] = torch.randn(D - 1, generator=g)           # one large entry alone
+    x = x.to(dtype)
+    w = (1 + 0.3 * torch.randn(D, generator=g)).to(dtype)
+    pos = torch.arange(9).int()[None]
+    freq = 10000.0 ** (-2.0 * torch.arange(rot // 2).double() / rot)
+    rope = ttf.TTFRope(freq.cuda(), layout=layout)
+    for eps in (0.0, 1e-35, 1e-6):
+        got, _ = ttf.ttf_qk_norm_rope(x.cuda(), None, pos.cuda(), rope, q_weight=w.cuda(), eps=eps)
+        eps = float(torch.tensor(eps))                      # (fp32, as the call takes it)
+        want, slack = norm_rotate(x, w, eps, pos, freq, None, layout, 1.0)
+        # results below the normal numbers of the type are off by up to half of its least step besides
+        check(got, want, slack + 2.0 ** -134, dtype, f"eps {eps}")
