@@ -376,7 +376,9 @@ ttf_status ttf_cache_append(const ttf_qk_params* params, const ttf_kv_cache* cac
  *   out = sum_u w_u v_u,  w = softmax_u(scale <q, k_u>),   lse = ln sum_u exp(scale <q, k_u>)
  * (lse joins parts of a context attended to separately).  A row that sees nothing gets out = 0, lse = -inf.  Query head h reads
  * key head h / (heads / kv_heads).  Entries that a row does not see have no influence on it, whatever bits
- * they hold.  Ordinary decoding is the chunk of one row: ttf_decode_alignment's position is cached[b], its mask
+ * they hold.  Scores, statistics and sums are in 32 bits.  With bf16, the weights of the sum over v_u are rounded on the way into the matrix
+ * cores: to 2^-16 of each, or, where max_rows heads / kv_heads is above 32 (16 with heads of more than 128 entries), to bf16 (2^-8 of each); lse
+ * is not touched by that.  Ordinary decoding is the chunk of one row: ttf_decode_alignment's position is cached[b], its mask
  * length the number of entries seen.
  *   max_rows    most rows of a sequence, or any other number from 1 on (below the mean it counts as the mean): it picks the kernel, and
  *               so the order of sums and the room in the workspace; no result depends on its being right

@@ -292,13 +292,21 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
                 }
         }
         if constexpr (E == 2) {
-            bf16x8 weight[NM];
+            // The weights as two bf16 values each, the second what the first leaves: with one, its rounding adds to that of the output (64 tokens over
+            // up to 32000 entries: rms error 1.81e-3 with one, 1.78e-3 with two, as much as rounding the exact output once).  Bytes bound these calls:
+            // the second product costs nothing there (the same tokens 776 us with one, 768 with two), 2 x 8 rows over 500 entries 12.4 -> 12.9 us.
+            bf16x8 weight[2][NM];
 #pragma unroll
             for (int n = 0; n < NM; ++n) {
-                u32x4 w;
+                u32x4 w[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = pack_bf16(s[n][e / 2][e % 2 * 2], s[n][e / 2][e % 2 * 2 + 1]);
-                weight[n] = __builtin_bit_cast(bf16x8, w);
+                for (int e = 0; e < 4; ++e) {
+                    const float x = s[n][e / 2][e % 2 * 2], y = s[n][e / 2][e % 2 * 2 + 1];
+                    w[0][e] = pack_bf16(x, y);
+                    w[1][e] = pack_bf16(x - __builtin_bit_cast(float, w[0][e] << 16), y - __builtin_bit_cast(float, w[0][e] & 0xffff0000u));
+                }
+                weight[0][n] = __builtin_bit_cast(bf16x8, w[0]);
+                weight[1][n] = __builtin_bit_cast(bf16x8, w[1]);
             }
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
@@ -307,8 +315,10 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
                 for (int e = 0; e < 4; ++e)
                     a[e] = __builtin_amdgcn_perm(v[2 * e + 1][i / 2], v[2 * e][i / 2], i % 2 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-                for (int n = 0; n < NM; ++n)
-                    o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), weight[n], o[n][i], 0, 0, 0);
+                for (int w = 0; w < 2; ++w)
+#pragma unroll
+                    for (int n = 0; n < NM; ++n)
+                        o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), weight[w][n], o[n][i], 0, 0, 0);
             }
         } else {
 #pragma unroll
@@ -323,6 +333,23 @@ __global__ __launch_bounds__(256, WAVES) void k_attend(ttf_attention_params p, t
             fetch_v(next);
             now = next;
         }
+    }
+
+    // An infinite value that met the second piece of a weight, which may be 0 or negative, is NaN now.  (NaN weights are not the values' doing.)
+    if constexpr (E == 2) {
+        bool odd = false;
+#pragma unroll
+        for (int n = 0; n < NM; ++n) {
+            f32x4 x = o[n][0];
+#pragma unroll
+            for (int i = 1; i < NI; ++i) x += o[n][i];
+            const float all = x[0] + x[1] + (x[2] + x[3]);
+            float l = sum[n];
+            l += __shfl_xor(l, 16, 64);
+            l += __shfl_xor(l, 32, 64);
+            odd |= all != all && l == l && limit[n] != 0x7fffffff;
+        }
+        tainted |= __ballot(odd) != 0;
     }
 
     // An infinite or NaN value that some rows see and others do not: 0 times it is no 0.  Rare, and done over again key by key
@@ -602,12 +629,14 @@ template <typename T, int DP, int NM>
 hipError_t launch(const ttf_attention_params& p, const ttf_kv_cache& c, const Choice& x, const Parts& w, hipStream_t s)
 {
     constexpr int WAVES = NM == 1 && DP * sizeof(T) <= 256 ? 3 : NM * DP * sizeof(T) <= 512 ? 2 : 1;
+    // (heads of 65 to 127 entries: a third wave spills, 32 tokens over 8000 entries of 72 172 us with three, 150 with two)
+    constexpr int CUT_WAVES = sizeof(T) == 2 && NM == 1 && DP == 128 ? 2 : WAVES;
     const unsigned grid = most_tiles(p, x) * p.kv_heads + x.target;
     const bool neighbours = x.neighbours && c.head_stride < c.slot_stride;      // (heads of a slot side by side)
     // (the offsets inside a tile are held in 32 bits)
     const auto go = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(p, c, x.columns, neighbours, x.target, w.out, w.stat, w.notes); };
-    if (c.page_size % 16 != 0 || c.slot_stride >= (1ll << 24)) go(k_attend<T, DP, NM, false, true, WAVES>);
-    else if (p.head_dim < DP) go(k_attend<T, DP, NM, true, true, WAVES>);
+    if (c.page_size % 16 != 0 || c.slot_stride >= (1ll << 24)) go(k_attend<T, DP, NM, false, true, CUT_WAVES>);
+    else if (p.head_dim < DP) go(k_attend<T, DP, NM, true, true, CUT_WAVES>);
     else go(k_attend<T, DP, NM, true, false, WAVES>);
     return hipGetLastError();
 }

@@ -343,6 +343,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
                 for (int r = 0; r < 16; ++r) s[t][r] = half[t] >> (8 * (r / 4) + r % 4) & 1 ? s[t][r] : -INFINITY;
         }
         // The weights against the maximum so far; where they get large, or there is none, against the block's own over again.
+        // Each is rounded to one bf16 value for its product, half a step of 2^-8 of it; their sum is not.  A second value for what the first leaves
+        // would make the output as good as rounded once (8 clips of up to 3600 rows: rms error 1.88e-3 with one, 1.68e-3 with two), but the
+        // matrix cores bound this kernel: 387 -> 495 us there, 4 x 512 rows over 8192 entries 162 -> 205 us.
         bf16x8 w[4];
         float added;
         bool last = false;

@@ -149,3 +149,46 @@ def test_norms_of_heads_whose_squares_leave_the_range(D, rot, layout, dtype):
         want, slack = norm_rotate(x, w, eps, pos, freq, None, layout, 1.0)
         # results below the normal numbers of the type are off by up to half of its least step besides
         check(got, want, slack + 2.0 ** -134, dtype, f"eps {eps}")
+
+
+@pytest.mark.parametrize("rows,cached,heads,kv_heads,D,page", [
+    ([1], [900], 32, 8, 128, 16),
+    ([1, 2, 1], [3000, 41, 700], 8, 2, 64, 16),
+    ([3, 1], [700, 2000], 8, 1, 128, 16),        # 24 columns
+    ([2, 1], [600, 90], 6, 2, 72, 16),
+    ([1, 1], [600, 1500], 4, 4, 80, 24),
+    ([2], [1100], 8, 2, 200, 16),
+    ([1], [1100], 4, 2, 256, 10),
+])
+def test_few_rows_round_their_output_alone(rows, cached, heads, kv_heads, D, page):
+    """bf16: a weight goes into the second product as two bf16 values, half a step of the second off, 2^-16 of it at most; sums are in
+    32 bits, and the output is rounded once."""
+    q, k, v, table, ks, vs = _problem(rows, cached, heads, kv_heads, D, page, BF)
+    out, _ = _run_attention(q, k, v, table, rows, cached, max_rows=max(rows))
+    first = 0
+    for b, (r, c) in enumerate(zip(rows, cached)):
+        seen, part = seen_mask(r, c, r + c, True, 0, torch.ones(r + c, dtype=torch.bool)), q[first:first + r].float()
+        want, _, slack, _ = attend(part, ks[b].float(), vs[b].float(), seen, D ** -0.5)
+        size, _, _, _ = attend(part, ks[b].float(), vs[b].float().abs(), seen, D ** -0.5)
+        check(out[first:first + r], want, slack + 2.0 ** -16 * (1 + 2.0 ** -8) * size, BF, f"sequence {b}")
+        first += r
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,cached,bad", [([1], [300], 40), ([1, 2], [3000, 20], 700), ([4], [90], 92), ([100], [300], 70), ([100], [300], 350)])
+def test_an_infinite_value_stays_infinite(rows, cached, bad, dtype):
+    """Values of inf and -inf, each in an entry of its own, with weights that do not underflow: the output is infinite likewise."""
+    q, k, v, table, ks, vs = _problem(rows, cached, 4, 2, 64, 16, dtype, peak=0.3)
+    for entry, value in ((7, math.inf), (20, -math.inf)):
+        vs[0][bad, :, entry] = v[int(table[0, bad // 16]), bad % 16, :, entry] = value
+    out, lse = _run_attention(q, k, v, table, rows, cached, max_rows=max(rows))
+    sees = cached[0] + torch.arange(rows[0]) >= bad
+    assert bool(sees.any()) and bool((out[:rows[0]][sees][..., 7] == math.inf).all()) and bool((out[:rows[0]][sees][..., 20] == -math.inf).all())
+    assert not bool(torch.isnan(out).any()) and bool(torch.isfinite(lse).all())
+    out[:rows[0]][..., [7, 20]] = 0.0
+    for b in range(len(vs)):
+        vs[b][..., [7, 20]] = 0.0
+    assert bool(torch.isfinite(out[:rows[0]]).all())
+    for x in {0, rows[0] // 2, rows[0] - 1}:
+        want, _, slack, _ = attend(q[x:x + 1], ks[0], vs[0], seen_mask(rows[0], cached[0], len(ks[0]), True, 0, torch.ones(len(ks[0]), dtype=torch.bool))[x:x + 1], 0.125)
+        check(out[x:x + 1], want, slack, dtype, f"row {x}")
