@@ -30,7 +30,7 @@ ttf_status check_rows(const void* p, int64_t row, int64_t head, int rows, int he
 // check_rows leaves them: at least D where there are two.)
 bool folded(int64_t row, int64_t head, int rows, int heads, int D)
 {
-    if (rows < 2 || heads < 2 || row >= (heads - 1) * head + D || head >= (rows - 1) * row + D) return false;
+    if (rows < 2 || heads < 2 || (row - D) / head >= heads - 1 || (head - D) / row >= rows - 1) return false;    // (one inside the other)
     for (int64_t j = 1; j < heads; ++j)
         for (int64_t i = j * head / row, end = i + 1; i <= end && i < rows; ++i)
             if (std::llabs(j * head - i * row) < D) return true;

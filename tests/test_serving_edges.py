@@ -107,3 +107,12 @@ def test_append_refuses_a_cache_whose_heads_overlap(slot, head):
         assert lib.ttf_cache_append(ctypes.byref(_qk()), ctypes.byref(c), None) == INVALID
     # reading such a cache is harmless
     assert lib.ttf_paged_attention(ctypes.byref(_attention()), ctypes.byref(c), A, 0, None) == SMALL
+
+
+def test_layouts_that_overlap_are_found_far_apart_too():
+    """Strides whose products with the sizes pass 63 bits."""
+    lib, far = serving._library(), 1 << 40
+    p = _attention(rows=1 << 24, heads=8, kv_heads=2, out=2 * A, o_row=far, o_head=far)
+    assert lib.ttf_paged_attention(ctypes.byref(p), ctypes.byref(_cache()), A, 0, None) == INVALID
+    p = _attention(rows=1 << 24, heads=8, kv_heads=2, out=2 * A, o_row=far, o_head=64)
+    assert lib.ttf_paged_attention(ctypes.byref(p), ctypes.byref(_cache()), A, 0, None) == SMALL
