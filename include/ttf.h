@@ -381,7 +381,7 @@ ttf_status ttf_cache_append(const ttf_qk_params* params, const ttf_kv_cache* cac
  * is not touched by that.  Ordinary decoding is the chunk of one row: ttf_decode_alignment's position is cached[b], its mask
  * length the number of entries seen.
  *   max_rows    most rows of a sequence, or any other number from 1 on (below the mean it counts as the mean): it picks the kernel, and
- *               so the order of sums and the room in the workspace; no result depends on its being right
+ *               so the order of sums, the rounding of weights and the room in the workspace; no result depends on its being right
  *   workspace   DEVICE, ttf_attention_workspace_size() bytes, 256-byte aligned; contents on entry do not matter.  Calls that may
  *               overlap need one each.  The size is enough for every call with the same dtype, head_dim, heads and kv_heads and
  *               no more rows, batch and max_rows: small calls may take more room than large ones, so a call by itself may need less

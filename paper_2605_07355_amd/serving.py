@@ -45,11 +45,19 @@ class _AttentionParams(ctypes.Structure):
 
 
 def _packer(structure):
-    """Packs the fields of a ctypes structure, in order, into bytes of its layout (several times faster than filling it)."""
+    """Packs the fields of a ctypes structure, in order, into bytes of its layout (several times faster than filling it, which
+    would also cut off numbers of more bits than a field has)."""
     codes = {_i32: "i", _i64: "q", _vp: "P", _f32: "f"}
     layout = "@" + "".join(codes[kind] for _, kind in structure._fields_)
     pad = ctypes.sizeof(structure) - struct.calcsize(layout)
-    return struct.Struct(layout + (f"{pad}x" if pad else "")).pack
+    pack = struct.Struct(layout + (f"{pad}x" if pad else "")).pack
+
+    def checked(*values):
+        try:
+            return pack(*values)
+        except (struct.error, OverflowError) as error:
+            raise ValueError(f"an argument is no number or does not fit its field: {error}") from None
+    return checked
 
 
 _pack_qk, _pack_cache, _pack_attention = _packer(_QKParams), _packer(_KVCache), _packer(_AttentionParams)
@@ -72,10 +80,10 @@ def _library():
     return _lib
 
 
-def _dtype_of(x: torch.Tensor) -> int:
-    code = _DTYPES.get(x.dtype)
+def _dtype_code(dtype: torch.dtype) -> int:
+    code = _DTYPES.get(dtype)
     if code is None:
-        raise TypeError(f"expected bfloat16 or float32, got {x.dtype}")
+        raise TypeError(f"expected bfloat16 or float32, got {dtype}")
     return code
 
 
@@ -203,7 +211,7 @@ def _qk_params(q, k, v, q_out, k_out, pos, rope, q_weight, k_weight, eps, row_of
     if ref is None or ref.dim() != 3:
         raise ValueError("q and k must be [rows, heads, head_dim]")
     (rows, _, D), dtype, gpu = ref.shape, ref.dtype, ref.get_device()
-    code = _dtype_of(ref)
+    code = _dtype_code(ref.dtype)
     qs, qo, ks, ko, vs = _NONE, _NONE, _NONE, _NONE, _NONE
     if q is not None:
         qs, qo = _heads("q", q, rows, D, dtype, gpu), _heads("q_out", q_out, rows, D, dtype, gpu)
@@ -287,9 +295,10 @@ def ttf_attention_workspace_size(rows: int, batch: int, heads: int, kv_heads: in
                                  dtype: torch.dtype = torch.bfloat16, max_rows: Optional[int] = None) -> int:
     """Bytes of workspace that ``ttf_paged_attention`` needs for such a call, and for every one with the same heads, head_dim and
     dtype and no more rows, sequences and ``max_rows`` (default: all rows)."""
-    p = _AttentionParams(_DTYPES[dtype], head_dim, heads, kv_heads, rows, batch, rows if max_rows is None else max_rows, 1, 0, 1.0)
+    packed = _pack_attention(_dtype_code(dtype), head_dim, heads, kv_heads, rows, batch, rows if max_rows is None else max_rows, 1, 0, 1.0,
+                             *(0,) * 9)
     n = ctypes.c_size_t(0)
-    _check(_library().ttf_attention_workspace_size(ctypes.byref(p), ctypes.byref(n)))
+    _check(_library().ttf_attention_workspace_size(packed, ctypes.byref(n)))
     return int(n.value)
 
 
@@ -318,7 +327,7 @@ def ttf_paged_attention(q: torch.Tensor, cache: TTFKVCache, row_offsets: torch.T
                             or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 [rows, heads] tensor on the device of q")
     batch = cache._batch
-    packed = _pack_attention(_dtype_of(q), D, heads, cache._heads, rows, batch, rows if max_rows is None else max_rows,
+    packed = _pack_attention(_dtype_code(q.dtype), D, heads, cache._heads, rows, batch, rows if max_rows is None else max_rows,
                              1 if causal else 0, window, D ** -0.5 if scale is None else scale,
                              _vector("row_offsets", row_offsets, batch + 1, torch.int32, gpu),
                              _vector("cached", cached, batch, torch.int32, gpu),

@@ -116,3 +116,21 @@ def test_layouts_that_overlap_are_found_far_apart_too():
     assert lib.ttf_paged_attention(ctypes.byref(p), ctypes.byref(_cache()), A, 0, None) == INVALID
     p = _attention(rows=1 << 24, heads=8, kv_heads=2, out=2 * A, o_row=far, o_head=64)
     assert lib.ttf_paged_attention(ctypes.byref(p), ctypes.byref(_cache()), A, 0, None) == SMALL
+
+
+def test_numbers_that_do_not_fit_their_fields_are_refused():
+    """2^32 + 5 rows are not 5 rows."""
+    for kw in (dict(rows=(1 << 32) + 5), dict(batch=1 << 32), dict(max_rows=1 << 31), dict(heads=(1 << 32) + 8), dict(head_dim=(1 << 32) + 64)):
+        args = dict(rows=8, batch=2, heads=8, kv_heads=2, head_dim=64) | kw
+        with pytest.raises(ValueError):
+            ttf.ttf_attention_workspace_size(**args)
+    with pytest.raises(TypeError):
+        ttf.ttf_attention_workspace_size(8, 2, 8, 2, 64, torch.float16)
+    x = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
+    k = torch.zeros((3, 16, 2, 64), dtype=torch.bfloat16)
+    cache, offsets, cached = ttf.TTFKVCache(k, k.clone(), torch.zeros((2, 4), dtype=torch.int32)), torch.tensor([0, 2, 4]).int(), torch.tensor([0, 0]).int()
+    for kw in (dict(window=1 << 31), dict(max_rows=1 << 40), dict(scale="0.125")):
+        with pytest.raises(ValueError, match="field"):
+            ttf.ttf_paged_attention(x, cache, offsets, cached, **kw)
+    with pytest.raises(ttf.TTFError):                       # infinite in 32 bits
+        ttf.ttf_paged_attention(x, cache, offsets, cached, scale=1e300)
