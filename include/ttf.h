@@ -282,6 +282,7 @@ ttf_status ttf_regate(const ttf_params* params, const void* features, const floa
  *   - row_offsets has to be non-decreasing and start at 0 or later; entries beyond `rows` count as `rows`.  (With
  *     others the outputs are undefined.)  Rows outside [row_offsets[0], row_offsets[batch]) are left as they were.
  *   - cached[b] < 0: sequence b appends nothing, and its rows attend to nothing.
+ *   - The attention sees the entries below 2^31 - 2^20 of a sequence.
  *   - Page-table entries outside [0, pages) are pages that are not there (not yet given out, or given back behind a
  *     window), and so is everything beyond table_width: nothing is appended to them, and their keys are left out of the softmax.
  */

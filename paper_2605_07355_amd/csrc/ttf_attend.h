@@ -50,9 +50,10 @@ struct Deal {
     int note;              // its number among the tiles of more than one part
     Sequence seq;
 };
+// (Times in this file and beside it, without further word: bf16, 32 query heads on 8 of 128 entries, ragged batches of up to the sizes given.)
 // Whether no tile is cut into parts, and none joined, because table or window leave no long context: up to 512 entries, 256 in fp32 (8 clips
-// of up to 200 rows 31.6 -> 16.3 us, 64 tokens over up to 400 entries 27.2 -> 23.7; fp32, 10 x 15 rows over 200 29.8 -> 23.4, but one token
-// over 400 20 -> 38).
+// of 200 rows 28.5 us cut, 14.8 not, 64 tokens over 400 entries 25.7 and 21.6; fp32, 10 x 15 rows over 200 27.0 and 21.0, but one token over 400
+// 15.1 and 17.6).  It goes by the room in the table, which the host knows, and not by the lengths.
 __host__ __device__ inline bool uncut(const ttf_attention_params& p, const ttf_kv_cache& c)
 {
     const long long room = (long long)c.page_size * c.table_width;
@@ -84,7 +85,7 @@ __device__ __forceinline__ int tiles_of(int rows, int group, int columns)
 // round of them.  64 lengths are tried, a lane each, from half of an even `share` on, for the least sum of the rounds' longest parts and
 // what a part costs besides (kPartTurns: its start, and its rows to the workspace and back; 5 and 14 choose alike).  At most 2 target
 // workgroups, or the share stays.  `tiles` and `turns`: of sequence `lane`, at most 64 of them.
-//   2000 rows over 31k keys 600 -> 512 us, 300 over 100k 361 -> 268 us, 4 x 128 rows over 8k keys 80 -> 64 us, 20 rows 37.1 -> 38.2 us
+//   with the even share and here: 300 rows over 100k keys 779 and 558 us, 4 x 128 over 8k 73 and 56, 2000 over 31k 1057 and 1029, 20 over 8k 23.6 and 24.3
 constexpr float kPartTurns = 9.0f;
 __device__ inline int even_turns(int batch, int kv_heads, int target, double share, int per, int tiles, int turns)
 {
@@ -133,8 +134,8 @@ __device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cach
     // a part of `per` turns: per blocks of one wave and four heads, or 4 per blocks of four waves and one head
     const double share = total * p.kv_heads / (4.0 * target);
     int per = __builtin_amdgcn_readfirstlane(share < 1.0 ? 1 : share > 1e9 ? 1000000000 : (int)__builtin_ceil(share));
-    // few rows: parts of up to 3 turns where a third of the workgroups is left then (8 tokens over 3000 entries 24.4 -> 22.3 us, 12 over a
-    // window of 8192 entries as before; fp32, 2 x 184 rows 73 -> 51 us)
+    // few rows: parts of up to 3 turns where a third of the workgroups is left then (8 tokens over 3000 entries 23.3 us with shorter ones, 20.8; 12 over a
+    // window of 8192 entries 39.3 either way)
     if (!even) per = max(per, __builtin_amdgcn_readfirstlane((int)__builtin_fmin(3.0, __builtin_ceil(3.0 * share))));
     if (even && p.batch <= 64) per = even_turns(p.batch, p.kv_heads, target, share, per, tiles, (blocks + 3) >> 2);
     d.heads = neighbours && per >= kNeighbourTurns ? kNeighbours : 1;
@@ -145,8 +146,8 @@ __device__ inline bool deal_out(const ttf_attention_params& p, const ttf_kv_cach
     for (int i = 0; i < p.batch; i += 64) {
         if (p.batch > 64) look(i);
         const int turns = (int)((unsigned)(blocks + waves - 1) / (unsigned)waves);
-        // One column's parts are joined one after the other: of a long context they get longer with its root (one token over 16796 entries
-        // of two key heads 24.2 -> 18.3 us, over 10^6 of one 235 -> 121 us, with the join in quarters)
+        // One column's parts are joined one after the other: of a long context they get longer with its root (one token over 10^6 entries of one
+        // key head 127 us without, 119 with; over 16796 of two 16.3 and 16.2)
         const int least = even ? per : max(per, (int)__builtin_amdgcn_sqrtf(0.03f * turns));
         const int parts = whole || turns == 0 ? 1 : (int)((unsigned)(turns + least - 1) / (unsigned)least), mine = tiles * parts;
         const int upto = units + wave_prefix(mine), held = parts > 1 ? mine : 0, notes_held = parts > 1 ? tiles : 0;

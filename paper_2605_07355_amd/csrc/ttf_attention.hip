@@ -56,7 +56,8 @@ __device__ __forceinline__ float share_of(float m, float most)
     return m == -INFINITY ? 0.0f : fmaxf(__builtin_amdgcn_exp2f(m - most), 0x1p-126f);
 }
 
-// Keys and values are read once a call as a rule: non-temporal (window of 8192 over 12 sequences 43.9 -> 39.8 us).
+// Keys and values are read once a call as a rule: non-temporal (64 tokens over 32000 entries 834 us without, 768 with; a window of 8192 over 12
+// sequences 37 and 39).
 template <typename V>
 __device__ __forceinline__ V load_once(const char* p) { return __builtin_nontemporal_load(reinterpret_cast<const V*>(p)); }
 
@@ -586,8 +587,9 @@ Choice choose(const ttf_attention_params& p, long long pairs)
 {
     Choice x{};
     x.width = p.head_dim <= 64 ? 64 : p.head_dim <= 128 ? 128 : 256;
-    // Between 17 and 32 columns either kernel may win with heads of up to 128 entries (32 x 8 rows over 8000 entries 124 us with few, 117 with many; 64 x 6 over
-    // 400 20 and 28); with 256 the one for few spills (475 and 370 us, 82 and 80).
+    // Between 17 and 32 columns either kernel may win with heads of up to 128 entries (32 x 8 rows over 8000 entries 138 us with the one for few, 131 with that
+    // for many; 64 x 6 over 400 24 and 32, 16 x 5 over 3000 the same); with 256, 16 columns are all that the one for few has registers for (16 heads on 4,
+    // 32 x 8 rows over 8000 entries 237 and 146 us).
     x.wide = p.dtype == TTF_BF16 && pairs > (x.width == 256 ? 16 : 32);
     if (x.wide) {
         x.columns = 128;
@@ -595,7 +597,8 @@ Choice choose(const ttf_attention_params& p, long long pairs)
         x.slots = 2 * x.target;
         return x;
     }
-    x.tiles = pairs <= 16 ? 1 : (pairs <= 32 || p.dtype == TTF_BF16 || x.width > 64) ? 2 : 4;    // (fp32 of 128 entries: four spill, 20 x 29 rows over 14k keys 945 us, two 779)
+    // (fp32 of 128 entries: four spill, 20 x 29 rows over 14000 keys 887 us, two 787)
+    x.tiles = pairs <= 16 ? 1 : (pairs <= 32 || p.dtype == TTF_BF16 || x.width > 64) ? 2 : 4;
     if (x.width == 256 && p.dtype == TTF_F32) x.tiles = 1;
     x.columns = pairs < 16 * x.tiles ? (int)pairs : 16 * x.tiles;    // no more than there are: the parts' rows take that much less room
     x.neighbours = p.kv_heads % kNeighbours == 0;
@@ -645,7 +648,7 @@ template <typename T>
 hipError_t launch_join(const ttf_attention_params& p, const Choice& x, const Parts& w, hipStream_t s)
 {
     // Few columns: a workgroup to each.  More: a wave to each.  Many tiles, few of which are cut as a rule: up to four to a wave (20 rows
-    // over 8192 entries 38.4 us with four, 33.0 with two, 30.8 with one; 8 clips of up to 1000 rows 61.1, 61.2, 63.4 us).
+    // over 8192 entries 24 us with one, 41 with four; 8 clips of 1000 rows 60 and 57, 4 x 512 rows over 8192 entries 166 and 159).
     const unsigned tiles = most_tiles(p, x) * p.kv_heads;
     const int each = x.columns <= 16 ? 0 : tiles <= 256 ? 1 : tiles <= 512 ? 2 : 4;
     const dim3 grid(tiles < (unsigned)x.slots / 2 ? tiles : (unsigned)x.slots / 2, (unsigned)(each ? (x.columns + 4 * each - 1) / (4 * each) : x.columns));
@@ -653,7 +656,7 @@ hipError_t launch_join(const ttf_attention_params& p, const Choice& x, const Par
         kernel<<<grid, 256, 0, s>>>(p, x.columns, each, x.slots, w.out, w.stat, w.notes);
         return hipGetLastError();
     };
-    // Where there are many tiles, each is in few parts (4 x 512 rows over 8192 entries, two to four: eight at once 25 us, four 22 us).
+    // Where there are many tiles, each is in few parts (4 x 512 rows over 8192 entries, two to four: with eight on their way 162 us, with four 159).
     if (each > 1) return x.width == 64 ? go(k_attend_join<T, 1, 4>) : x.width == 128 ? go(k_attend_join<T, 2, 4>) : go(k_attend_join<T, 4, 4>);
     return x.width == 64 ? go(k_attend_join<T, 1, 8>) : x.width == 128 ? go(k_attend_join<T, 2, 8>) : go(k_attend_join<T, 4, 8>);
 }

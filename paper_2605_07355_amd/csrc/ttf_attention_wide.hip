@@ -298,16 +298,16 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_wide(ttf_atte
 
     bf16x8 q[KS];
     // Block at place `at` of the buffer.  The next block's loads are spread over its first products: issued all at once they hold
-    // up the waves until the last is taken (2000 rows over 31k keys: 728 us, spread out 598 us, before the parts came in whole rounds).
-    // Of a SIMD's two waves the one that multiplies goes first, the other takes its weights in between (8 clips of up to 3600 rows 407 -> 384 us,
-    // the other way round 392; with one wave a SIMD it only costs).
+    // up the waves until the last is taken (2000 rows over 31k keys 1086 us, spread out 1030; 8 clips of 3600 rows 396 and 379).
+    // Of a SIMD's two waves the one that multiplies goes first, the other takes its weights in between (the same clips 397 us without, 382 with,
+    // 394 the other way round; with one wave a SIMD it only costs).
     const auto first = [&](bool it) {
         if constexpr (DP == 256) return;
         if (it) __builtin_amdgcn_s_setprio(1);
         else __builtin_amdgcn_s_setprio(0);
     };
-    // Operands are read from LDS four products with K, three with V ahead (the same clips 403 -> 381 us, heads of 256 entries 1160 -> 980 us against
-    // the compiler's own order).
+    // Operands are read from LDS four products with K, three with V ahead (the same clips 398 us in the compiler's own order, 387 so; 16 heads of 256
+    // entries on 4 547 and 512).
     const auto work = [&](int at, int to, int base, bool gaps) {
         const int kp = hide(k_place + at), vp = hide(v_place + at);
         first(true);

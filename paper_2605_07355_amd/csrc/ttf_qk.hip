@@ -27,7 +27,7 @@ template <> struct Word<4> { typedef uint32_t type; };
 template <> struct Word<2> { typedef uint16_t type; };
 
 // V elements from memory into fp32 and back (rounded to nearest even), in one access of V * sizeof(T) bytes.  Written without a place in the
-// caches (16 clips 132 -> 122 us, two 26 -> 21; reading likewise gains 3 % there and loses 19 % on two clips).
+// caches (16 clips 122 us with one, 116 so, two clips 20 either way; reading likewise 115 on the 16, but 23 on the two).
 template <typename T, int V>
 __device__ __forceinline__ void load_chunk(const T* p, float* v)
 {
@@ -217,7 +217,7 @@ hipError_t launch(const ttf_qk_params& p, const ttf_kv_cache* cache, hipStream_t
     while (group * UNITS < units) group *= 2;
     const int per = 64 / group, all = p.heads + p.kv_heads * (cache ? 2 : 1), rounds = (all + per - 1) / per;
     // Two waves share the heads of a row, more where that leaves the chip empty.  Every one of them forms the angles, but has less to wait for (16
-    // clips of up to 3600 rows 122 us with one, 118 with two, 131 with five; appended 148, 141, 172).
+    // clips of up to 3600 rows 115.5 us with one, 115 with two, 125 with four; appended 145, 139, 152).
     int shares = 1;
     while (shares * 2 <= rounds && (shares < 2 || (long long)p.rows * shares < 2048)) shares *= 2;
     const long long waves = (long long)p.rows * shares;

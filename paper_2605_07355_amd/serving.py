@@ -1,5 +1,8 @@
 """ctypes binding of the entry points behind the compressed rows (see ``include/ttf.h``): norm and
-rotation of queries and keys, cache append, attention over a paged cache.  Argument marshalling only."""
+rotation of queries and keys, cache append, attention over a paged cache.  Argument marshalling only.
+
+For inference: nothing is kept for a backward pass.  Outputs carry no gradient, also where an input requires one, and what is
+written in place (``q_out``, ``k_out``, ``out``, ``lse``, the cache) changes without autograd's knowledge."""
 from __future__ import annotations
 
 import ctypes
@@ -262,7 +265,7 @@ def ttf_qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: 
     and ``k`` [rows, kv_heads, D], either of which may be None, by the positions ``pos`` int32 [axes, rows].
 
     ``row_offsets`` [batch + 1] (as ``ttf_compress`` writes it): only its rows are worked on, rows behind the
-    last sequence stay as they were.  ``q_out`` / ``k_out`` may be the inputs themselves.  Returns (q_out, k_out)."""
+    last sequence stay as they were.  ``q_out`` / ``k_out`` may be the inputs themselves.  Returns (q_out, k_out).  No gradients."""
     if q is not None and q_out is None:
         q_out = _empty(q.shape, q.dtype, q.device, stream)
     if k is not None and k_out is None:
@@ -280,7 +283,7 @@ def ttf_cache_append(cache: TTFKVCache, k: torch.Tensor, v: torch.Tensor, row_of
                      q_weight: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                      stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
     """Put normed and rotated keys and the values of packed rows into ``cache``: row i of sequence b becomes entry
-    ``cached[b] + i``.  ``q`` is normed and rotated in the same launch.  Returns q_out (None without q)."""
+    ``cached[b] + i``.  ``q`` is normed and rotated in the same launch.  Returns q_out (None without q).  No gradients."""
     if cache._k.dtype is not k.dtype or cache._gpu != k.get_device() or (cache._heads, cache._head_dim) != tuple(k.shape[1:]):
         raise ValueError("the cache must have the heads, head_dim, dtype and device of k")
     if q is not None and q_out is None:
@@ -311,7 +314,7 @@ def ttf_paged_attention(q: torch.Tensor, cache: TTFKVCache, row_offsets: torch.T
     rows' own (``ttf_cache_append`` first).  ``max_rows`` (most rows of one sequence, at least 1; default: all) picks the kernel
     and with it the room taken in ``workspace`` (uint8, of ttf_attention_workspace_size; taken from torch where not given);
     ``scale`` defaults to 1/sqrt(D); ``window`` > 0: a row looks back over that many entries, itself included; ``lse``
-    float32 [rows, heads] is filled where given.  Rows outside ``row_offsets`` stay as they were."""
+    float32 [rows, heads] is filled where given.  Rows outside ``row_offsets`` stay as they were.  No gradients."""
     if q.dim() != 3:
         raise ValueError("q must be [rows, heads, head_dim]")
     (rows, heads, D), dtype, gpu = q.shape, q.dtype, q.get_device()
